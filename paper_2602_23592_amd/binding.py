@@ -22,6 +22,11 @@ KEEP_BUDGET_GROUP_COUNT, KEEP_BUDGET_TOKENS = 0, 1
 KEEP_LOAD_SERIAL, KEEP_LOAD_NEXT_LAYER, KEEP_LOAD_LAYER_BALANCED = 0, 1, 2
 KEEP_KERNELS_AUTO, KEEP_KERNELS_GENERIC = 0, 1
 KEEP_REPORT_MAX_LAYERS = 128
+KEEP_ROPE_HALF, KEEP_ROPE_INTERLEAVED = 0, 1
+KEEP_ROPE_PLAIN, KEEP_ROPE_LINEAR, KEEP_ROPE_BASE, KEEP_ROPE_PARTS = 0, 1, 2, 3
+KEEP_CACHE_F32, KEEP_CACHE_BF16, KEEP_CACHE_FP8, KEEP_CACHE_INT8 = 0, 1, 2, 3
+KEEP_PAGED_MAX_SEQS = 4096
+KEEP_SAMPLE_MAX_VOCAB = 1 << 20
 
 KEEP_OPT_PROPAGATION_SOURCES = 0
 KEEP_SOURCES_QUERY_AND_SET, KEEP_SOURCES_SET_ONLY = 0, 1
@@ -33,6 +38,9 @@ EXPORTED = ("keep_init", "keep_destroy", "keep_last_error", "keep_uses_mfma", "k
             "keep_score_groups", "keep_select_groups", "keep_prefill",
             "keep_prefill_padded", "keep_decode", "keep_precompute_group", "keep_precompute_groups",
             "keep_dequantize_int4", "keep_attach_int4",
+            "keep_rope_frequencies", "keep_rope_rows", "keep_cache_write", "keep_cache_read",
+            "keep_paged_attention_workspace_bytes", "keep_paged_attention", "keep_sample_workspace_bytes", "keep_sample",
+            "keep_decode_sampled",
             "keep_memory_create", "keep_memory_destroy", "keep_memory_last_error",
             "keep_memory_put", "keep_memory_remove", "keep_memory_end_step", "keep_memory_unit_count",
             "keep_memory_unit_info", "keep_memory_unit_tokens", "keep_memory_mark_computed")
@@ -86,6 +94,37 @@ class Report(C.Structure):
                  ("attn_rows", C.c_int32 * _L), ("attn_keys", C.c_uint64 * _L)]
                 + [(_n, C.c_float * _L) for _n in _REPORT_MS]
                 + [("bytes_loaded", C.c_uint64 * _L)])
+
+
+class RopeDesc(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("scaling", C.c_int32), ("theta", C.c_double), ("factor", C.c_double),
+                ("trained_len", C.c_int32), ("fast", C.c_double), ("slow", C.c_double)]
+
+
+class RopeRowsDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "n_rows", "n_q_heads", "n_kv_heads", "head_dim", "rot_dim", "layout")] + \
+               [("magnitude", C.c_float)] + \
+               [(n, C.c_int64) for n in ("q_in_stride", "q_out_stride", "k_in_stride", "k_out_stride")]
+
+
+class PagedCacheDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("format", "n_pages", "page_size", "n_kv_heads", "head_dim")] + \
+               [(n, C.c_int64) for n in ("page_stride", "head_stride", "token_stride")] + \
+               [(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale")]
+
+
+class PagedAttentionDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "n_seqs", "n_rows", "n_q_heads", "max_pages", "window")] + \
+               [("scale", C.c_float), ("q_stride", C.c_int64), ("out_stride", C.c_int64)]
+
+
+class SampleDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "n_rows", "vocab")] + [("row_stride", C.c_int64)]
+
+
+class Sampling(C.Structure):
+    _fields_ = [("temperature", C.c_float), ("top_k", C.c_int32), ("top_p", C.c_float), ("min_p", C.c_float),
+                ("uniform", C.POINTER(C.c_float))]
 
 
 _lib = None
@@ -150,6 +189,25 @@ def load_library() -> C.CDLL:
     lib.keep_dequantize_int4.argtypes = [vp, vp, i32, i32, vp, vp]
     lib.keep_attach_int4.restype = i32
     lib.keep_attach_int4.argtypes = [vp, C.POINTER(LayerWeightsInt4)]
+    lib.keep_rope_frequencies.restype = i32
+    lib.keep_rope_frequencies.argtypes = [C.POINTER(RopeDesc), C.POINTER(C.c_double), C.POINTER(f32)]
+    lib.keep_rope_rows.restype = i32
+    lib.keep_rope_rows.argtypes = [C.POINTER(RopeRowsDesc), vp, vp, vp, vp, vp, vp, vp]
+    for name in ("keep_cache_write", "keep_cache_read"):
+        getattr(lib, name).restype = i32
+        getattr(lib, name).argtypes = [C.POINTER(PagedCacheDesc), i32, vp, vp, i32, C.c_int64, vp, vp]
+    lib.keep_paged_attention_workspace_bytes.restype = C.c_uint64
+    lib.keep_paged_attention_workspace_bytes.argtypes = [C.POINTER(PagedCacheDesc), i32, i32]
+    lib.keep_paged_attention.restype = i32
+    lib.keep_paged_attention.argtypes = [C.POINTER(PagedAttentionDesc), C.POINTER(PagedCacheDesc), vp, vp, vp, vp, vp, vp, vp,
+                                         C.c_uint64, vp]
+    lib.keep_sample_workspace_bytes.restype = C.c_uint64
+    lib.keep_sample_workspace_bytes.argtypes = [i32, i32]
+    lib.keep_sample.restype = i32
+    lib.keep_sample.argtypes = [C.POINTER(SampleDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp, C.c_uint64, vp]
+    lib.keep_decode_sampled.restype = i32
+    lib.keep_decode_sampled.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, C.POINTER(Sampling), pi32, C.POINTER(f32), vp,
+                                        pi32]
     lib.keep_precompute_group.restype = i32
     lib.keep_precompute_group.argtypes = [vp, pi32, i32, vp, vp, C.POINTER(Report)]
     lib.keep_precompute_groups.restype = i32
@@ -265,6 +323,196 @@ def select_groups_static(S: torch.Tensor, groups: torch.Tensor, group_len: torch
                                        _stream_handle(stream if stream is not None else torch.cuda.current_stream()))
     if st != KEEP_OK:
         raise KeepError(st, lib.keep_last_error(None).decode())
+
+
+# ---- the operators of include/keep_serve.h ------------------------------------------------------------------
+_DTYPES = {torch.float32: KEEP_F32, torch.bfloat16: KEEP_BF16}
+_FORMATS = {torch.float32: KEEP_CACHE_F32, torch.bfloat16: KEEP_CACHE_BF16, torch.float8_e4m3fn: KEEP_CACHE_FP8,
+            torch.int8: KEEP_CACHE_INT8}
+
+
+def _refuse(text: str):
+    raise KeepError(KEEP_ERR_INVALID_ARG, text)
+
+
+def _launch(device: torch.device, stream, call, *args):
+    """One call on `stream`, by default the current one of the tensors' device, with that device current."""
+    with torch.cuda.device(device):
+        st = call(*args, _stream_handle(stream if stream is not None else torch.cuda.current_stream(device)))
+    if st != KEEP_OK:
+        raise KeepError(st, _lib.keep_last_error(None).decode())
+
+
+def _array(name: str, t: Optional[torch.Tensor], dtype, numel: int, device: torch.device, optional: bool = False):
+    """Address of a dense device array of `numel` elements"""
+    if t is None:
+        return None if optional else _refuse(name + " is missing")
+    if t.dtype != dtype or t.numel() != numel or not t.is_contiguous() or t.device != device:
+        _refuse("%s must be a dense %s array of %d elements on %s" % (name, dtype, numel, device))
+    return t.data_ptr()
+
+
+def _heads(name: str, t: torch.Tensor, device: torch.device, dtype=None) -> int:
+    """Row stride of [rows, heads, head_dim] whose rows are dense"""
+    if t.dim() != 3 or t.device != device or t.dtype not in _DTYPES or (dtype is not None and t.dtype != dtype):
+        _refuse("%s must be [rows, heads, head_dim] in float32 or bfloat16, of one type and on one device" % name)
+    rows, h, d = t.shape
+    if not (t.numel() == 0 or ((d == 1 or t.stride(2) == 1) and (h == 1 or t.stride(1) == d))):
+        _refuse("the heads of a row of %s must be adjacent" % name)
+    return t.stride(0) if rows > 1 else h * d
+
+
+def rope_frequencies(rot_dim: int, theta: float = 1.0e6, scaling: int = KEEP_ROPE_PLAIN, factor: float = 1.0,
+                     trained_len: int = 1, fast: float = 32.0, slow: float = 1.0):
+    """keep_rope_frequencies: (float64 numpy array [rot_dim / 2], factor on the rotated values)"""
+    lib = load_library()
+    freq = np.zeros(max(1, rot_dim // 2), dtype=np.float64)
+    mag = C.c_float(0.0)
+    desc = RopeDesc(rot_dim, scaling, theta, factor, trained_len, fast, slow)
+    st = lib.keep_rope_frequencies(C.byref(desc), freq.ctypes.data_as(C.POINTER(C.c_double)), C.byref(mag))
+    if st != KEEP_OK:
+        raise KeepError(st, lib.keep_last_error(None).decode())
+    return freq, mag.value
+
+
+def rope_rows(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: torch.Tensor, freq: torch.Tensor,
+              layout: int = KEEP_ROPE_HALF, magnitude: float = 1.0, q_out: Optional[torch.Tensor] = None,
+              k_out: Optional[torch.Tensor] = None, stream=None):
+    """keep_rope_rows: q, k [rows, heads, head_dim] (either may be None) -> q_out, k_out, by default q and k themselves.
+    rot_dim is twice the length of freq (float64, on the device)."""
+    lib = load_library()
+    ref = q if q is not None else k
+    if ref is None:
+        _refuse("neither queries nor keys")
+    q_out, k_out = q if q_out is None else q_out, k if k_out is None else k_out
+    n, d = ref.shape[0], ref.shape[-1]
+    strides = []
+    for name, t in (("q", q), ("q_out", q_out), ("k", k), ("k_out", k_out)):
+        if t is None:
+            strides.append(0)
+            continue
+        strides.append(_heads(name, t, ref.device, ref.dtype))
+        if t.shape[0] != n or t.shape[2] != d:
+            _refuse("rows or head_dim of %s differ" % name)
+    if (q_out is not None and (q is None or q_out.shape != q.shape)) or (k_out is not None and (k is None or k_out.shape != k.shape)):
+        _refuse("an output's shape differs from its input's")
+    desc = RopeRowsDesc(_DTYPES[ref.dtype], n, 0 if q is None else q.shape[1], 0 if k is None else k.shape[1], d,
+                        2 * freq.numel(), layout, magnitude, *strides)
+    _launch(ref.device, stream, lib.keep_rope_rows, C.byref(desc), _ptr(q), _ptr(q_out), _ptr(k), _ptr(k_out),
+            _array("positions", positions, torch.int32, n, ref.device),
+            _array("freq", freq, torch.float64, freq.numel(), ref.device))
+    return q_out, k_out
+
+
+class PagedCache:
+    """keep_paged_cache over tensors k, v [n_pages, n_kv_heads, page_size, head_dim] (float32, bfloat16, float8_e4m3fn or
+    int8; any strides with adjacent values) and, for the 8-bit types, float32 k_scale, v_scale [n_pages, n_kv_heads, page_size].
+    Keeps the tensors alive."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
+                 v_scale: Optional[torch.Tensor] = None):
+        self.lib = load_library()
+        if k.dim() != 4 or k.dtype not in _FORMATS or v.shape != k.shape or v.dtype != k.dtype or v.stride() != k.stride() \
+                or v.device != k.device or not k.is_cuda:
+            _refuse("k and v must be alike, [n_pages, n_kv_heads, page_size, head_dim], of a cache type, on the GPU")
+        if k.stride(3) != 1:
+            _refuse("a head's values must be adjacent")
+        n = k.shape[0] * k.shape[1] * k.shape[2]
+        scaled = k.element_size() == 1
+        if not scaled and (k_scale is not None or v_scale is not None):
+            _refuse("only 8-bit caches have scales")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.device = k.device
+        self.c = PagedCacheDesc(_FORMATS[k.dtype], k.shape[0], k.shape[2], k.shape[1], k.shape[3], k.stride(0), k.stride(1),
+                                k.stride(2), k.data_ptr(), v.data_ptr(),
+                                _array("k_scale", k_scale, torch.float32, n, k.device, not scaled),
+                                _array("v_scale", v_scale, torch.float32, n, k.device, not scaled))
+
+    @classmethod
+    def empty(cls, dtype: torch.dtype, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, device="cuda"):
+        """A cache of new, uninitialised dense pages"""
+        shape = (n_pages, n_kv_heads, page_size, head_dim)
+        k, v = (torch.empty(shape, dtype=dtype, device=device) for _ in range(2))
+        ks, vs = (torch.empty(shape[:3], dtype=torch.float32, device=device) if k.element_size() == 1 else None
+                  for _ in range(2))
+        return cls(k, v, ks, vs)
+
+    def _rows(self, call, k, v, slots, stream):
+        stride = _heads("k", k, self.device)
+        if _heads("v", v, self.device, k.dtype) != stride or v.shape != k.shape or \
+                tuple(k.shape[1:]) != (self.c.n_kv_heads, self.c.head_dim):
+            _refuse("k and v must be alike, [rows, n_kv_heads, head_dim]")
+        _launch(self.device, stream, call, C.byref(self.c), _DTYPES[k.dtype], k.data_ptr(), v.data_ptr(), k.shape[0], stride,
+                _array("slots", slots, torch.int32, k.shape[0], self.device))
+
+    def write(self, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, stream=None):
+        """keep_cache_write: rows k, v [n, n_kv_heads, head_dim] into the slots (int32 [n])"""
+        self._rows(self.lib.keep_cache_write, k, v, slots, stream)
+
+    def read(self, slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, stream=None):
+        """keep_cache_read: the slots' rows into k, v [n, n_kv_heads, head_dim]"""
+        self._rows(self.lib.keep_cache_read, k, v, slots, stream)
+
+
+def paged_attention_workspace_bytes(n_q_heads: int, cache: PagedCache, n_seqs: int) -> int:
+    return int(cache.lib.keep_paged_attention_workspace_bytes(C.byref(cache.c), n_q_heads, n_seqs))
+
+
+def paged_attention(q: torch.Tensor, cache: PagedCache, q_start: torch.Tensor, kv_len: torch.Tensor,
+                    page_table: torch.Tensor, window: int = 0, scale: float = 0.0, out: Optional[torch.Tensor] = None,
+                    lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """keep_paged_attention: q [rows, n_q_heads, head_dim] of len(kv_len) sequences, rows q_start[s] .. q_start[s + 1] each,
+    page_table int32 [n_seqs, max_pages].  out and workspace (uint8) are allocated where they are not given."""
+    stride = _heads("q", q, cache.device)
+    n, hq, d = q.shape
+    if d != cache.c.head_dim:
+        _refuse("head_dim of q differs from the cache's")
+    seqs = kv_len.numel()
+    if page_table.dim() != 2 or page_table.shape[0] != seqs:
+        _refuse("page_table must be [n_seqs, max_pages]")
+    if out is None:
+        out = torch.empty((n, hq, d), dtype=q.dtype, device=q.device)
+    if out.shape != q.shape:
+        _refuse("out must have the shape of q")
+    need = paged_attention_workspace_bytes(hq, cache, seqs)
+    if workspace is None:
+        workspace = torch.empty(max(1, need), dtype=torch.uint8, device=q.device)
+    desc = PagedAttentionDesc(_DTYPES[q.dtype], seqs, n, hq, page_table.shape[1], window, scale, stride,
+                              _heads("out", out, q.device, q.dtype))
+    dev = cache.device
+    _launch(dev, stream, cache.lib.keep_paged_attention, C.byref(desc), C.byref(cache.c), q.data_ptr(),
+            _array("q_start", q_start, torch.int32, seqs + 1, dev), _array("kv_len", kv_len, torch.int32, seqs, dev),
+            _array("page_table", page_table, torch.int32, page_table.numel(), dev), out.data_ptr(),
+            _array("lse", lse, torch.float32, n * hq, dev, True),
+            _array("workspace", workspace, torch.uint8, workspace.numel(), dev), workspace.numel())
+    return out
+
+
+def sample_workspace_bytes(n_rows: int, vocab: int) -> int:
+    return int(load_library().keep_sample_workspace_bytes(n_rows, vocab))
+
+
+def sample(logits: torch.Tensor, uniform: torch.Tensor, temperature: Optional[torch.Tensor] = None,
+           top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None,
+           tokens: Optional[torch.Tensor] = None, probs: Optional[torch.Tensor] = None,
+           workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """keep_sample: one token per row of logits [rows, vocab], from uniform [rows]; the parameters are arrays [rows]."""
+    lib = load_library()
+    if logits.dim() != 2 or logits.dtype not in _DTYPES or (logits.numel() and logits.shape[1] > 1 and logits.stride(1) != 1):
+        _refuse("logits must be [rows, vocab] in float32 or bfloat16 with adjacent values")
+    n, vocab = logits.shape
+    dev = logits.device
+    if tokens is None:
+        tokens = torch.empty(n, dtype=torch.int32, device=dev)
+    if workspace is None:
+        workspace = torch.empty(max(1, sample_workspace_bytes(n, vocab)), dtype=torch.uint8, device=dev)
+    desc = SampleDesc(_DTYPES[logits.dtype], n, vocab, logits.stride(0) if n > 1 else vocab)
+    _launch(dev, stream, lib.keep_sample, C.byref(desc), logits.data_ptr(), _array("uniform", uniform, torch.float32, n, dev),
+            _array("temperature", temperature, torch.float32, n, dev, True), _array("top_k", top_k, torch.int32, n, dev, True),
+            _array("top_p", top_p, torch.float32, n, dev, True), _array("min_p", min_p, torch.float32, n, dev, True),
+            _array("tokens", tokens, torch.int32, n, dev), _array("probs", probs, torch.float32, n, dev, True),
+            _array("workspace", workspace, torch.uint8, workspace.numel(), dev), workspace.numel())
+    return tokens
 
 
 class KeepContext:
@@ -461,6 +709,24 @@ class KeepContext:
                                          k_cache.data_ptr(), v_cache.data_ptr(), k_cache.shape[1], n_ctx, n_new,
                                          out.ctypes.data_as(C.POINTER(C.c_int32)), _ptr(logits_out), fp))
         return [int(v) for v in out[:n_new]]
+
+    def decode_sampled(self, final_norm: torch.Tensor, lm_head: torch.Tensor, x_last: torch.Tensor, k_cache: torch.Tensor,
+                       v_cache: torch.Tensor, n_ctx: int, uniform: Sequence[float], temperature: float = 1.0, top_k: int = 0,
+                       top_p: float = 1.0, min_p: float = 0.0, logits_out: Optional[torch.Tensor] = None,
+                       forced_tokens: Optional[Sequence[int]] = None):
+        """keep_decode_sampled: one token per uniform number; returns (tokens, their probabilities)"""
+        u = np.ascontiguousarray(np.asarray(uniform, dtype=np.float32))
+        n_new = len(u)
+        out, probs = np.zeros(max(1, n_new), dtype=np.int32), np.zeros(max(1, n_new), dtype=np.float32)
+        fp = None
+        if forced_tokens is not None:
+            f, fp = _i32_array(list(forced_tokens) if len(forced_tokens) else [0])
+        how = Sampling(temperature, top_k, top_p, min_p, u.ctypes.data_as(C.POINTER(C.c_float)))
+        self._check(self.lib.keep_decode_sampled(
+            self.handle, final_norm.data_ptr(), lm_head.data_ptr(), x_last.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+            k_cache.shape[1], n_ctx, n_new, C.byref(how), out.ctypes.data_as(C.POINTER(C.c_int32)),
+            probs.ctypes.data_as(C.POINTER(C.c_float)), _ptr(logits_out), fp))
+        return [int(v) for v in out[:n_new]], [float(v) for v in probs[:n_new]]
 
     def precompute_group(self, token_ids: Sequence[int], k_blocks: torch.Tensor, v_blocks: torch.Tensor,
                          want_report: bool = False):

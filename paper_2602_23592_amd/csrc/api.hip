@@ -14,6 +14,7 @@
 
 #include "keep_internal.h"
 #include "keep_memory.h"
+#include "keep_serve.h"
 
 using namespace keep;
 
@@ -88,7 +89,7 @@ struct keep_ctx {
   bool set_only = false;            // KEEP_OPT_PROPAGATION_SOURCES = KEEP_SOURCES_SET_ONLY
   bool ev_light = false;            // record only the events around the gate/up GEMM (keep_report.events_in = 1)
   bool units_mode = false;          // rows attend only from their unit's first row on
-  int32_t* h_dec = nullptr;         // pinned [4 * KEEP_DECODE_MAX_TOKENS]: positions, fed tokens, results
+  int32_t* h_dec = nullptr;         // pinned [6 * KEEP_DECODE_MAX_TOKENS]: positions, fed tokens, results, zero, uniforms, probabilities
   int32_t* d_dec = nullptr;         // device mirror
   float* dec_logits = nullptr;      // [vocab]
   uint64_t* argmax_part = nullptr;  // [ARGMAX_BLOCKS]
@@ -120,6 +121,9 @@ namespace {
 }  // namespace
 
 namespace keep {
+// sample.hip: one row of fp32 logits; how->uniform is not read (d_uniform: DEVICE), a row without a number gives token 0
+void launch_sample_decode(const float* logits, int32_t vocab, const float* d_uniform, const keep_sampling& how, int32_t* token,
+                          float* prob, hipStream_t s);
 // message behind keep_last_error(NULL), for entry points that have no context
 void set_init_error(const char* text) { g_init_error = text; }
 }  // namespace keep
@@ -253,7 +257,7 @@ uint64_t workspace_bytes(const keep_model_desc* d) {
   t += align256((z.G + 1) * z.G * sizeof(float));                      // S
   t += align256(select_scratch_words((int32_t)z.G) * sizeof(float));   // sel_scratch
   t += align256((z.G + 2) * sizeof(int32_t));                          // sel_out
-  t += align256(4 * KEEP_DECODE_MAX_TOKENS * 4) + align256((size_t)d->vocab * sizeof(float));  // decode
+  t += align256(6 * KEEP_DECODE_MAX_TOKENS * 4) + align256((size_t)d->vocab * sizeof(float));  // decode
   t += align256(ARGMAX_BLOCKS * sizeof(uint64_t));
   t += 2 * align256(z.M * sizeof(int32_t));                            // row_lo, row_list
   t += 3 * align256(z.M * sizeof(int32_t));                            // token deviation, flags, kept list
@@ -671,11 +675,12 @@ keep_status by_dtype(keep_ctx* c, F&& f) {
 template <typename T>
 keep_status decode_impl(keep_ctx* c, const void* final_norm, const void* lm_head, const void* x_last, void* k_cache,
                         void* v_cache, int32_t cache_rows, int32_t n_ctx, int32_t n_new, int32_t* tokens_out,
-                        float* logits_out, const int32_t* forced_tokens) {
+                        float* logits_out, const int32_t* forced_tokens, const keep_sampling* how, float* probs_out) {
   const keep_model_desc& d = c->d;
   hipStream_t s = c->s_comp;
   constexpr int CAP = KEEP_DECODE_MAX_TOKENS;
-  // pinned / device ints: [0, CAP) positions, [CAP, 2 CAP) fed tokens (forced), [2 CAP, 3 CAP) results, [3 CAP] zero
+  // pinned / device ints: [0, CAP) positions, [CAP, 2 CAP) fed tokens (forced), [2 CAP, 3 CAP) results, [3 CAP] zero,
+  // and as floats [4 CAP, 5 CAP) uniform numbers, [5 CAP, 6 CAP) probabilities of the drawn tokens
   int32_t* h = c->h_dec;
   for (int t = 0; t < CAP; ++t) {
     h[t] = n_ctx + t;
@@ -683,7 +688,13 @@ keep_status decode_impl(keep_ctx* c, const void* final_norm, const void* lm_head
     h[2 * CAP + t] = 0;
   }
   h[3 * CAP] = 0;
-  HIP_TRY(c, hipMemcpyAsync(c->d_dec, h, (size_t)(3 * CAP + 1) * 4, hipMemcpyHostToDevice, s));
+  size_t up = 3 * CAP + 1;
+  if (how) {
+    memcpy(h + 4 * CAP, how->uniform, (size_t)n_new * 4);
+    up = 5 * CAP;
+  }
+  float* d_float = reinterpret_cast<float*>(c->d_dec);
+  HIP_TRY(c, hipMemcpyAsync(c->d_dec, h, up * 4, hipMemcpyHostToDevice, s));
   const size_t row_bytes = (size_t)d.n_kv_heads * d.head_dim * c->esz;
   const size_t layer_bytes = (size_t)cache_rows * row_bytes;
   GemmB bh{};
@@ -713,7 +724,10 @@ keep_status decode_impl(keep_ctx* c, const void* final_norm, const void* lm_head
                        EPI_STORE_F32, nullptr, lg, s, c->skinny_ws, nullptr, head_norm ? &final_rn : nullptr);
     else
       launch_gemm_generic<T>(Typed<T>::p(c->hbuf), 1, d.hidden, bh, nullptr, d.vocab, EPI_STORE_F32, nullptr, lg, s);
-    launch_argmax(lg, d.vocab, c->d_dec + 2 * CAP + t, c->argmax_part, s);
+    if (how)
+      launch_sample_decode(lg, d.vocab, d_float + 4 * CAP + t, *how, c->d_dec + 2 * CAP + t, d_float + 5 * CAP + t, s);
+    else
+      launch_argmax(lg, d.vocab, c->d_dec + 2 * CAP + t, c->argmax_part, s);
     HIP_TRY(c, hipGetLastError());
     if (t + 1 == n_new) break;
     // the chosen (or forced) token at position n_ctx + t through every layer
@@ -781,9 +795,40 @@ keep_status decode_impl(keep_ctx* c, const void* final_norm, const void* lm_head
     x = x_cur;
   }
   HIP_TRY(c, hipMemcpyAsync(h + 2 * CAP, c->d_dec + 2 * CAP, (size_t)n_new * 4, hipMemcpyDeviceToHost, s));
+  if (how && probs_out)
+    HIP_TRY(c, hipMemcpyAsync(h + 5 * CAP, c->d_dec + 5 * CAP, (size_t)n_new * 4, hipMemcpyDeviceToHost, s));
   HIP_TRY(c, hipStreamSynchronize(s));
   for (int t = 0; t < n_new; ++t) tokens_out[t] = h[2 * CAP + t];
+  if (how && probs_out) memcpy(probs_out, h + 5 * CAP, (size_t)n_new * 4);
   return KEEP_OK;
+}
+
+// keep_decode and keep_decode_sampled (sampling not NULL)
+keep_status decode_checked(keep_ctx* c, const void* final_norm, const void* lm_head, const void* x_last, void* k_cache,
+                           void* v_cache, int32_t cache_rows, int32_t n_ctx, int32_t n_new, int32_t* tokens_out,
+                           float* logits_out, const int32_t* forced_tokens, const keep_sampling* sampling,
+                           float* probs_out) {
+  if (!c) return KEEP_ERR_INVALID_ARG;
+  if (!final_norm || !lm_head || !x_last || !k_cache || !v_cache || !tokens_out)
+    return fail(c, KEEP_ERR_INVALID_ARG, "final_norm / lm_head / x_last / k_cache / v_cache / tokens_out is NULL");
+  if (n_new < 1 || n_new > KEEP_DECODE_MAX_TOKENS)
+    return fail(c, KEEP_ERR_INVALID_ARG, "n_new %d outside [1, %d]", n_new, KEEP_DECODE_MAX_TOKENS);
+  if (n_ctx < 1) return fail(c, KEEP_ERR_INVALID_ARG, "n_ctx must be at least 1");
+  if ((int64_t)n_ctx + n_new - 1 > cache_rows)
+    return fail(c, KEEP_ERR_INVALID_ARG, "n_ctx + n_new - 1 = %lld rows do not fit cache_rows %d",
+                (long long)n_ctx + n_new - 1, cache_rows);
+  if ((int64_t)n_ctx + n_new - 1 > c->d.max_tokens)
+    return fail(c, KEEP_ERR_WORKSPACE, "n_ctx + n_new - 1 above max_tokens %d", c->d.max_tokens);
+  if (forced_tokens)
+    for (int t = 0; t + 1 < n_new; ++t)
+      if (forced_tokens[t] < 0 || forced_tokens[t] >= c->d.vocab)
+        return fail(c, KEEP_ERR_INVALID_ARG, "forced_tokens[%d] = %d outside the vocabulary", t, forced_tokens[t]);
+  c->last_layer = -1;
+  return by_dtype(c, [&](auto* tag) {
+    using T = std::remove_pointer_t<decltype(tag)>;
+    return decode_impl<T>(c, final_norm, lm_head, x_last, k_cache, v_cache, cache_rows, n_ctx, n_new, tokens_out, logits_out,
+                          forced_tokens, sampling, probs_out);
+  });
 }
 
 }  // namespace
@@ -954,7 +999,7 @@ keep_status keep_init(const keep_model_desc* desc, const keep_layer_weights* lay
     TRY_INIT(mk());
   }
   TRY_INIT(pin_alloc(c, &c->h_sel_out, (z.G + 2) * 4));
-  TRY_INIT(pin_alloc(c, &c->h_dec, 4 * KEEP_DECODE_MAX_TOKENS * 4));
+  TRY_INIT(pin_alloc(c, &c->h_dec, 6 * KEEP_DECODE_MAX_TOKENS * 4));
   TRY_INIT(pin_alloc(c, &c->h_row_lo, z.M * 4));
   TRY_INIT(pin_alloc(c, &c->h_row_list, z.M * 4));
   TRY_INIT(dev_alloc(c, &c->d_row_list, z.M * 4));
@@ -971,7 +1016,7 @@ keep_status keep_init(const keep_model_desc* desc, const keep_layer_weights* lay
   TRY_INIT(dev_alloc(c, &c->d_tok_list, z.M * 4));
   TRY_INIT(pin_alloc(c, &c->h_tok_list, z.M * 4));
   TRY_INIT(pin_alloc(c, &c->h_dev, z.M * 4));
-  TRY_INIT(dev_alloc(c, &c->d_dec, 4 * KEEP_DECODE_MAX_TOKENS * 4));
+  TRY_INIT(dev_alloc(c, &c->d_dec, 6 * KEEP_DECODE_MAX_TOKENS * 4));
   TRY_INIT(dev_alloc(c, &c->dec_logits, (size_t)desc->vocab * sizeof(float)));
   TRY_INIT(dev_alloc(c, &c->argmax_part, ARGMAX_BLOCKS * sizeof(uint64_t)));
   TRY_INIT(pin_alloc(c, &c->h_S, (z.G + 1) * z.G * sizeof(float)));
@@ -1329,27 +1374,25 @@ keep_status keep_select_tokens(keep_ctx* c, const float* deviation, int32_t n, i
 keep_status keep_decode(keep_ctx* c, const void* final_norm, const void* lm_head, const void* x_last, void* k_cache,
                         void* v_cache, int32_t cache_rows, int32_t n_ctx, int32_t n_new, int32_t* tokens_out,
                         float* logits_out, const int32_t* forced_tokens) {
+  return decode_checked(c, final_norm, lm_head, x_last, k_cache, v_cache, cache_rows, n_ctx, n_new, tokens_out, logits_out,
+                        forced_tokens, nullptr, nullptr);
+}
+
+keep_status keep_decode_sampled(keep_ctx* c, const void* final_norm, const void* lm_head, const void* x_last, void* k_cache,
+                                void* v_cache, int32_t cache_rows, int32_t n_ctx, int32_t n_new,
+                                const keep_sampling* sampling, int32_t* tokens_out, float* probs_out, float* logits_out,
+                                const int32_t* forced_tokens) {
   if (!c) return KEEP_ERR_INVALID_ARG;
-  if (!final_norm || !lm_head || !x_last || !k_cache || !v_cache || !tokens_out)
-    return fail(c, KEEP_ERR_INVALID_ARG, "final_norm / lm_head / x_last / k_cache / v_cache / tokens_out is NULL");
-  if (n_new < 1 || n_new > KEEP_DECODE_MAX_TOKENS)
-    return fail(c, KEEP_ERR_INVALID_ARG, "n_new %d outside [1, %d]", n_new, KEEP_DECODE_MAX_TOKENS);
-  if (n_ctx < 1) return fail(c, KEEP_ERR_INVALID_ARG, "n_ctx must be at least 1");
-  if ((int64_t)n_ctx + n_new - 1 > cache_rows)
-    return fail(c, KEEP_ERR_INVALID_ARG, "n_ctx + n_new - 1 = %lld rows do not fit cache_rows %d",
-                (long long)n_ctx + n_new - 1, cache_rows);
-  if ((int64_t)n_ctx + n_new - 1 > c->d.max_tokens)
-    return fail(c, KEEP_ERR_WORKSPACE, "n_ctx + n_new - 1 above max_tokens %d", c->d.max_tokens);
-  if (forced_tokens)
-    for (int t = 0; t + 1 < n_new; ++t)
-      if (forced_tokens[t] < 0 || forced_tokens[t] >= c->d.vocab)
-        return fail(c, KEEP_ERR_INVALID_ARG, "forced_tokens[%d] = %d outside the vocabulary", t, forced_tokens[t]);
-  c->last_layer = -1;
-  return by_dtype(c, [&](auto* tag) {
-    using T = std::remove_pointer_t<decltype(tag)>;
-    return decode_impl<T>(c, final_norm, lm_head, x_last, k_cache, v_cache, cache_rows, n_ctx, n_new, tokens_out,
-                          logits_out, forced_tokens);
-  });
+  if (!sampling || !sampling->uniform) return fail(c, KEEP_ERR_INVALID_ARG, "sampling / uniform is NULL");
+  if (!isfinite(sampling->temperature) || !isfinite(sampling->top_p) || !isfinite(sampling->min_p))
+    return fail(c, KEEP_ERR_INVALID_ARG, "temperature, top_p or min_p is not finite");
+  if (c->d.vocab > KEEP_SAMPLE_MAX_VOCAB)
+    return fail(c, KEEP_ERR_SHAPE, "vocabulary of %d is above %d", c->d.vocab, KEEP_SAMPLE_MAX_VOCAB);
+  for (int t = 0; t < n_new && t < KEEP_DECODE_MAX_TOKENS; ++t)
+    if (!(sampling->uniform[t] >= 0.f && sampling->uniform[t] < 1.f))
+      return fail(c, KEEP_ERR_INVALID_ARG, "uniform[%d] is outside [0, 1)", t);
+  return decode_checked(c, final_norm, lm_head, x_last, k_cache, v_cache, cache_rows, n_ctx, n_new, tokens_out, logits_out,
+                        forced_tokens, sampling, probs_out);
 }
 
 keep_status keep_dequantize_int4(const void* codes, const void* scale_zero, int32_t rows, int32_t K, void* out,

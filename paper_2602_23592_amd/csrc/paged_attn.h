@@ -1,0 +1,192 @@
+// What the kernels of paged attention share: arguments, the division of a launch's work, partial results.
+//
+// Work.  A job is (sequence, key/value head, tile of TR query rows); a query row is a token paired with one of the head's query
+// heads.  A job takes as many units as it has key tiles of KT keys between the first key its rows may see and the
+// last, at least one (so that rows which see nothing are written too).  All units of a launch, in the order sequence,
+// head, tile, key, are dealt to the workers (workgroups; no more than there are units) in equal runs: lengths differ by orders of magnitude from
+// sequence to sequence, and their division has to come from device memory, where a captured graph finds the
+// step's own.  Every worker forms the division for itself: sums per sequence in LDS, a scan, then its own place.
+//
+// A job cut by a border between runs leaves one partial result per worker: unnormalised output, running maximum and sum.  A
+// worker cuts at most the job it begins with (slot 2 w) and the one it ends with (slot 2 w + 1); the worker a cut job begins in
+// leaves a record, by which k_paged_join adds the parts in the order of their keys.
+#pragma once
+#include "serve_common.h"
+
+namespace keep {
+
+constexpr int PAGED_WORKERS = 512;  // two workgroups for each of 256 CUs
+
+struct PagedRecord {  // of a worker: the cut job that begins in it
+  int32_t seq, head, tile;
+  int32_t last;       // the last worker of that job; 0: no such job
+};
+
+struct PagedArgs {
+  keep_paged_cache c;
+  const void* q;
+  void* out;
+  float* lse;
+  const int32_t *q_start, *kv_len, *table;
+  int64_t q_stride, out_stride;
+  int n_seqs, n_rows, n_q_heads, rep, max_pages, window, capacity, dtype;
+  float scale_log2e;
+  FastDiv by_page, by_rep;
+  PagedRecord* rec;  // [PAGED_WORKERS]
+  float* part_ml;    // [2 PAGED_WORKERS][2][TR]: maximum (log2 domain), sum
+  float* part_o;     // [2 PAGED_WORKERS][head_dim / 4][TR][4]
+};
+
+struct PagedSeq {
+  int row0, rows, len;  // first query row, their number, tokens in the cache
+};
+
+__device__ __forceinline__ PagedSeq paged_seq(const PagedArgs& a, int s) {
+  PagedSeq q;
+  q.row0 = min(max(a.q_start[s], 0), a.n_rows);
+  q.rows = min(max(a.q_start[s + 1], q.row0), a.n_rows) - q.row0;
+  q.len = min(max(a.kv_len[s], 0), a.capacity);
+  return q;
+}
+
+// Key tiles of one tile of query rows: [first, first + units)
+template <int TR, int KT>
+__device__ __forceinline__ void paged_span(const PagedArgs& a, const PagedSeq& q, int tile, int& first, int& units) {
+  const int x1 = min(q.rows * a.rep, (tile + 1) * TR);
+  const int last = q.len - q.rows + (int)div_by(x1 - 1, a.by_rep);
+  const int from = q.len - q.rows + (int)div_by(tile * TR, a.by_rep);
+  first = a.window ? max(0, from - a.window + 1) / KT : 0;
+  units = last < 0 ? 1 : last / KT + 1 - first;
+  if (last < 0) first = 0;
+}
+template <int TR>
+__device__ __forceinline__ int paged_tiles(const PagedArgs& a, const PagedSeq& q) {
+  return (q.rows * a.rep + TR - 1) / TR;
+}
+
+// Every worker that takes part has a unit at least
+__device__ __forceinline__ uint64_t paged_workers(uint64_t total) { return min(total, (uint64_t)PAGED_WORKERS); }
+// The worker that takes unit v: the largest w with w * total / workers <= v
+__device__ __forceinline__ int paged_worker_of(uint64_t v, uint64_t total) {
+  return (int)(((v + 1) * paged_workers(total) - 1) / total);
+}
+
+struct PagedPlace {    // where a worker begins, and how far it goes
+  uint64_t total;      // units of the launch
+  uint64_t begin, end; // this worker's run
+  int seq, head, tile;
+  int unit;            // units of the first job that earlier workers take
+};
+
+// Called by all 256 threads; lds: 8 * (n_seqs + 260) bytes, free again after the caller's next barrier.
+template <int TR, int KT>
+__device__ __forceinline__ PagedPlace paged_place(const PagedArgs& a, int worker, uint64_t* lds) {
+  const int tid = threadIdx.x;
+  uint64_t* sums = lds + 260;
+  for (int s = tid; s < a.n_seqs; s += 256) sums[s] = 0;
+  __syncthreads();
+  // a few sequences: several threads add up the tiles of one; many: a thread takes every 256th
+  int share = 1;
+  while (share * 2 * a.n_seqs <= 256) share *= 2;
+  for (int s = tid / share; s < a.n_seqs; s += 256 / share) {
+    const PagedSeq q = paged_seq(a, s);
+    const int tiles = paged_tiles<TR>(a, q);
+    uint64_t sum = 0;
+    for (int t = tid % share; t < tiles; t += share) {
+      int first, units;
+      paged_span<TR, KT>(a, q, t, first, units);
+      sum += units;
+    }
+    if (sum) atomicAdd(reinterpret_cast<unsigned long long*>(sums + s), (unsigned long long)sum);
+  }
+  __syncthreads();
+  const int per = (a.n_seqs + 255) / 256;
+  const int s0 = min(tid * per, a.n_seqs), s1 = min(s0 + per, a.n_seqs);
+  uint64_t own = 0;
+  for (int s = s0; s < s1; ++s) own += sums[s];
+  uint64_t before = own;  // inclusive scan over the wave, then over the waves
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint64_t up = __shfl_up((unsigned long long)before, o, 64);
+    if ((tid & 63) >= o) before += up;
+  }
+  if ((tid & 63) == 63) lds[tid >> 6] = before;
+  __syncthreads();
+  uint64_t total = 0;
+  for (int w = 0; w < 4; ++w) {
+    if (w < (tid >> 6)) before += lds[w];
+    total += lds[w];
+  }
+  before -= own;
+  PagedPlace p;
+  p.total = total * a.c.n_kv_heads;
+  const uint64_t workers = paged_workers(p.total);
+  p.begin = p.end = p.total;
+  if ((uint64_t)worker < workers) {
+    p.begin = p.total * worker / workers;
+    p.end = p.total * (worker + 1) / workers;
+  }
+  if (tid == 0) lds[8] = 0, lds[9] = 0;
+  __syncthreads();
+  before *= a.c.n_kv_heads;
+  own *= a.c.n_kv_heads;
+  if (own && p.begin >= before && p.begin < before + own) {
+    int s = s0;
+    uint64_t at = p.begin - before;
+    while (at >= sums[s] * a.c.n_kv_heads) at -= sums[s++] * a.c.n_kv_heads;
+    lds[8] = s;
+    lds[9] = at;
+    lds[10] = sums[s];
+  }
+  __syncthreads();
+  p.seq = p.head = p.tile = p.unit = 0;
+  if (p.begin < p.end) {
+    p.seq = (int)lds[8];
+    p.head = (int)(lds[9] / lds[10]);
+    uint64_t at = lds[9] - p.head * lds[10];
+    // the tile: 64 at a time, a lane each
+    const PagedSeq q = paged_seq(a, p.seq);
+    const int tiles = paged_tiles<TR>(a, q), lane = tid & 63;
+    for (int t0 = 0;; t0 += 64) {
+      int first, units = 0;
+      if (t0 + lane < tiles) paged_span<TR, KT>(a, q, t0 + lane, first, units);
+      uint64_t sum = units;
+      for (int o = 1; o < 64; o <<= 1) {
+        const uint64_t up = __shfl_up((unsigned long long)sum, o, 64);
+        if (lane >= o) sum += up;
+      }
+      const uint64_t past = __ballot(sum > at);
+      if (past || t0 + 64 >= tiles) {
+        const int l = past ? __ffsll((unsigned long long)past) - 1 : 0;
+        p.tile = t0 + l;
+        p.unit = (int)(at - (l ? __shfl((unsigned long long)sum, l - 1, 64) : 0));
+        break;
+      }
+      at -= __shfl((unsigned long long)sum, 63, 64);
+    }
+  }
+  return p;
+}
+
+// The job behind (seq, head, tile); sequences without rows are passed over.  Only called where another job exists.
+template <int TR>
+__device__ __forceinline__ void paged_next(const PagedArgs& a, PagedPlace& p, PagedSeq& q) {
+  p.unit = 0;
+  if (++p.tile < paged_tiles<TR>(a, q)) return;
+  p.tile = 0;
+  if (++p.head < a.c.n_kv_heads) return;
+  p.head = 0;
+  do q = paged_seq(a, ++p.seq);
+  while (q.rows == 0 && p.seq + 1 < a.n_seqs);
+}
+
+// Element offset of key `key` of a sequence, head excluded
+__device__ __forceinline__ int64_t paged_key(const PagedArgs& a, const int32_t* table, int key, int64_t& scale) {
+  const int n = (int)div_by(key, a.by_page), at = key - n * a.c.page_size;
+  const int page = min(max(table[n], 0), a.c.n_pages - 1);
+  scale = (int64_t)page * a.c.n_kv_heads * a.c.page_size + at;
+  return page * a.c.page_stride + at * a.c.token_stride;
+}
+
+void launch_paged_generic(const PagedArgs& a, hipStream_t s);
+
+}  // namespace keep

@@ -1,0 +1,360 @@
+// Attention of new tokens over a cache in pages: the entry point, the join of cut jobs, and the kernel for every type and
+// head width (fp32 matrix instruction).  paged_attn.h says how the work is dealt.
+//
+// One pass over the keys with a running maximum m and sum l per query row (log2 domain):
+//   m' = max(m, s),  l' = l 2^(m - m') + sum 2^(s - m'),  O' = O 2^(m - m') + 2^(s - m') V,   result O / l.
+#include <algorithm>
+
+#include "paged_attn.h"
+
+namespace keep {
+namespace {
+
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+
+constexpr int GT_ROWS = 16, GT_KEYS = 64;
+
+__device__ __forceinline__ float load_value(const void* p, int64_t i, int dtype) {
+  return dtype == KEEP_F32 ? static_cast<const float*>(p)[i] : bf16_bits_to_f32(static_cast<const uint16_t*>(p)[i]);
+}
+
+// Four values of a cache from element i on, as the numbers they stand for
+__device__ __forceinline__ f32x4 load_cached(const void* p, int64_t i, int format, float scale) {
+  if (format == KEEP_CACHE_F32) return *reinterpret_cast<const f32x4*>(static_cast<const float*>(p) + i);
+  if (format == KEEP_CACHE_BF16) {
+    const uint2 u = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + i);
+    return f32x4{bf16_bits_to_f32((uint16_t)u.x), bf16_bits_to_f32((uint16_t)(u.x >> 16)),
+                 bf16_bits_to_f32((uint16_t)u.y), bf16_bits_to_f32((uint16_t)(u.y >> 16))};
+  }
+  const uint32_t u = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(p) + i);
+  if (format == KEEP_CACHE_FP8) {
+    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)u, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)u, true);
+    return f32x4{lo[0] * scale, lo[1] * scale, hi[0] * scale, hi[1] * scale};
+  }
+  return f32x4{(float)(int8_t)u * scale, (float)(int8_t)(u >> 8) * scale, (float)(int8_t)(u >> 16) * scale,
+               (float)(int8_t)(u >> 24) * scale};
+}
+
+__device__ __forceinline__ bool finite4(f32x4 v) {
+  bool ok = true;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) ok = ok && (__float_as_uint(v[e]) & 0x7f800000u) != 0x7f800000u;
+  return ok;
+}
+
+// Any types, head_dim a multiple of 16 up to 16 * ND.  A worker's tile is 16 query rows and 64 keys; each of the four waves takes
+// 16 of the keys for all rows, with statistics and output of its own, added at a job's end.  S^T = K . Q^T leaves a lane one
+// query row (lane % 16) and four keys (4 (lane / 16) + r), which is the operand that O^T = V^T . P^T wants from it in step r:
+// the probabilities never leave their registers.  Rows of K and V in LDS are padded by four values, so that both operand
+// reads meet all banks.
+template <int ND>
+__global__ void __launch_bounds__(256) k_paged_generic(PagedArgs a) {
+  extern __shared__ __attribute__((aligned(16))) float lds[];
+  __shared__ int odd;  // some value of the tile is not finite
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, g = lane >> 4;
+  const int dh = a.c.head_dim, nd = dh / 16, stride = dh + 4;
+  const int worker = blockIdx.x;
+  PagedPlace p = paged_place<GT_ROWS, GT_KEYS>(a, worker, reinterpret_cast<uint64_t*>(lds));
+  if (tid == 0) a.rec[worker].last = 0;
+  if (p.begin >= p.end) return;
+  float* sk = lds;
+  float* sv = lds + GT_KEYS * stride;
+  float* sml = sv + GT_KEYS * stride;  // [2][4 waves][16]
+  PagedSeq q = paged_seq(a, p.seq);
+  for (uint64_t at = p.begin;;) {
+    int first, units;
+    paged_span<GT_ROWS, GT_KEYS>(a, q, p.tile, first, units);
+    const int u0 = p.unit, u1 = (int)min((uint64_t)units, u0 + (p.end - at));
+    const int x = p.tile * GT_ROWS + col;
+    const bool valid = x < q.rows * a.rep;
+    const int token = valid ? (int)div_by(x, a.by_rep) : 0;
+    const int head = p.head * a.rep + (valid ? x - token * a.rep : 0);
+    const int pos = valid ? q.len - q.rows + token : -1;
+    const int lo = a.window ? max(0, pos - a.window + 1) : 0;
+    float qf[4 * ND];
+    const int64_t q_at = (int64_t)(q.row0 + token) * a.q_stride + (int64_t)head * dh + g * (dh / 4);
+#pragma unroll
+    for (int i = 0; i < 4 * ND; ++i) qf[i] = i < 4 * nd ? load_value(a.q, q_at + i, a.dtype) : 0.f;
+    f32x4 acc[ND];
+#pragma unroll
+    for (int i = 0; i < ND; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;
+    const int32_t* table = a.table + (int64_t)p.seq * a.max_pages;
+
+    for (int kt = first + u0; kt < first + u1; ++kt) {
+      __syncthreads();  // the tile before has been read
+      if (tid == 0) odd = 0;
+      __syncthreads();
+      bool ok = true;
+      for (int i = tid; i < GT_KEYS * (dh / 4); i += 256) {
+        const int row = i / (dh / 4), d = (i - row * (dh / 4)) * 4, key = kt * GT_KEYS + row;
+        f32x4 k{0.f, 0.f, 0.f, 0.f}, v = k;
+        if (key < q.len) {
+          int64_t sc;
+          const int64_t e = paged_key(a, table, key, sc) + p.head * a.c.head_stride + d;
+          sc += (int64_t)p.head * a.c.page_size;
+          const bool scaled = a.c.k_scale != nullptr;
+          k = load_cached(a.c.k, e, a.c.format, scaled ? a.c.k_scale[sc] : 1.f);
+          v = load_cached(a.c.v, e, a.c.format, scaled ? a.c.v_scale[sc] : 1.f);
+        }
+        ok = ok && finite4(v);
+        *reinterpret_cast<f32x4*>(sk + row * stride + d) = k;
+        *reinterpret_cast<f32x4*>(sv + row * stride + d) = v;
+      }
+      if (!ok) odd = 1;
+      __syncthreads();
+      const float* wk = sk + (wave * 16 + col) * stride + g * (dh / 4);
+      f32x4 s{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < ND; ++i) {
+        if (i >= nd) continue;
+        const f32x4 k = *reinterpret_cast<const f32x4*>(wk + 4 * i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k[e], qf[4 * i + e], s, 0, 0, 0);
+      }
+      const int key0 = kt * GT_KEYS + wave * 16;
+      float top = -INFINITY;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int key = key0 + 4 * g + r;
+        s[r] = key <= pos && key >= lo ? s[r] * a.scale_log2e : -INFINITY;
+        top = fmaxf(top, s[r]);
+      }
+      top = fmaxf(top, __shfl_xor(top, 16, 64));
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      const float m_new = fmaxf(m, top), m_ref = m_new == -INFINITY ? 0.f : m_new;
+      if (__ballot(m_new != m)) {
+        const float alpha = __builtin_amdgcn_exp2f(m - m_ref);
+        l *= alpha;
+#pragma unroll
+        for (int i = 0; i < ND; ++i) acc[i] *= alpha;
+        m = m_new;
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        s[r] = __builtin_amdgcn_exp2f(s[r] - m_ref);
+        l += s[r];
+      }
+      const float* wv = sv + (wave * 16) * stride;
+      if (!odd) {
+#pragma unroll
+        for (int i = 0; i < ND; ++i) {
+          if (i >= nd) continue;
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            acc[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(wv[(4 * g + r) * stride + 16 * i + col], s[r], acc[i], 0, 0, 0);
+        }
+      } else {
+        // a product with a probability of zero would carry infinities and NaN to rows that do not see the key
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const float pj = __shfl(s[j & 3], (j >> 2) * 16 + col, 64);
+          const bool sees = key0 + j <= pos && key0 + j >= lo;
+#pragma unroll
+          for (int i = 0; i < ND; ++i) {
+            if (i >= nd) continue;
+            const f32x4 v = *reinterpret_cast<const f32x4*>(wv + j * stride + 16 * i + 4 * g);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[i][r] += sees ? pj * v[r] : 0.f;
+          }
+        }
+      }
+    }
+
+    // ---- the four waves' parts, in their order
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    __syncthreads();
+    if (g == 0) sml[wave * 16 + col] = m, sml[64 + wave * 16 + col] = l;
+    float* so = lds;  // [4 waves][dh / 4][16][4]
+#pragma unroll
+    for (int i = 0; i < ND; ++i)
+      if (i < nd) *reinterpret_cast<f32x4*>(so + ((wave * (dh / 4) + 4 * i + g) * 16 + col) * 4) = acc[i];
+    __syncthreads();
+    const bool whole = u0 == 0 && u1 == units;
+    const int slot = 2 * worker + (u0 == 0 ? 1 : 0);
+    {
+      float mw[4], m_all = -INFINITY, l_all = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) m_all = fmaxf(m_all, mw[w] = sml[w * 16 + col]);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        mw[w] = mw[w] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw[w] - m_all);
+        l_all += sml[64 + w * 16 + col] * mw[w];
+      }
+      // (a thread keeps the query row of its lane: tid % 16 = col)
+      for (int d4 = tid >> 4; d4 < dh / 4; d4 += 16) {
+        f32x4 o{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const f32x4 v = *reinterpret_cast<const f32x4*>(so + ((w * (dh / 4) + d4) * 16 + col) * 4);
+          o += mw[w] == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : v * mw[w];
+        }
+        if (!whole) {
+          *reinterpret_cast<f32x4*>(a.part_o + (((int64_t)slot * (dh / 4) + d4) * GT_ROWS + col) * 4) = o;
+        } else if (valid) {
+          if (l_all != 0.f) o /= l_all;
+          const int64_t o_at = (int64_t)(q.row0 + token) * a.out_stride + (int64_t)head * dh + d4 * 4;
+          if (a.dtype == KEEP_F32)
+            *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + o_at) = o;
+          else
+            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + o_at) =
+                make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]));
+        }
+      }
+      if (tid < 16) {
+        if (!whole) {
+          a.part_ml[(slot * 2) * GT_ROWS + col] = m_all;
+          a.part_ml[(slot * 2 + 1) * GT_ROWS + col] = l_all;
+        } else if (valid && a.lse) {
+          a.lse[(int64_t)(q.row0 + token) * a.n_q_heads + head] = 0.6931471805599453f * (m_all + log2f(l_all));
+        }
+      }
+    }
+    if (tid == 0 && u0 == 0 && !whole)
+      a.rec[worker] = PagedRecord{p.seq, p.head, p.tile, paged_worker_of(at + units - 1, p.total)};
+    at += u1 - u0;
+    if (at >= p.end) break;
+    paged_next<GT_ROWS>(a, p, q);
+  }
+}
+
+// The parts of a job that was cut, joined in the order of their keys.  A workgroup takes the job that worker blockIdx.x left a
+// record of, and a quarter of the output's dimensions (blockIdx.y).  Threads lie along query rows, then along parts (as
+// many as there are, up to eight and while rows and parts fill a wave: a butterfly adds those), then along dimensions.
+template <int TR>
+__global__ void __launch_bounds__(256) k_paged_join(PagedArgs a) {
+  const PagedRecord r = a.rec[blockIdx.x];
+  if (r.last == 0) return;
+  const PagedSeq q = paged_seq(a, r.seq);
+  const int dh = a.c.head_dim, rows = min(TR, q.rows * a.rep - r.tile * TR), n = r.last - (int)blockIdx.x + 1;
+  int rb = 1, parts = 1;
+  while (rb < rows) rb *= 2;
+  while (parts < n && parts < 8 && 2 * parts * rb <= 64) parts *= 2;
+  const int row = threadIdx.x & (rb - 1), part = (threadIdx.x / rb) & (parts - 1), d0 = threadIdx.x / (rb * parts);
+  const int w0 = blockIdx.x;
+  const auto slot_of = [&](int i) { return i == 0 ? 2 * w0 + 1 : 2 * (w0 + i); };
+  float m = -INFINITY, l = 0.f;
+  for (int i = part; i < n; i += parts) m = fmaxf(m, a.part_ml[(slot_of(i) * 2) * TR + row]);
+  for (int o = rb; o < rb * parts; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  const float m_ref = m == -INFINITY ? 0.f : m;
+  for (int i = part; i < n; i += parts)
+    l += a.part_ml[(slot_of(i) * 2 + 1) * TR + row] * __builtin_amdgcn_exp2f(a.part_ml[(slot_of(i) * 2) * TR + row] - m_ref);
+  for (int o = rb; o < rb * parts; o <<= 1) l += __shfl_xor(l, o, 64);
+  const int x = r.tile * TR + row, token = (int)div_by(min(x, q.rows * a.rep - 1), a.by_rep);
+  const int head = r.head * a.rep + x - token * a.rep;
+  const float inv = l != 0.f ? 1.f / l : 0.f;
+  const int quarter = dh / 16;  // groups of four dimensions per workgroup
+  for (int d4 = blockIdx.y * quarter + d0; d4 < (blockIdx.y + 1) * quarter; d4 += 256 / (rb * parts)) {
+    f32x4 o{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int i = part; i < n; i += parts) {
+      const float w = __builtin_amdgcn_exp2f(a.part_ml[(slot_of(i) * 2) * TR + row] - m_ref);
+      const f32x4 v = *reinterpret_cast<const f32x4*>(a.part_o + (((int64_t)slot_of(i) * (dh / 4) + d4) * TR + row) * 4);
+      o += w == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : v * w;
+    }
+    for (int s = rb; s < rb * parts; s <<= 1)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], s, 64);
+    if (part != 0 || row >= rows) continue;
+    o *= inv;
+    const int64_t o_at = (int64_t)(q.row0 + token) * a.out_stride + (int64_t)head * dh + d4 * 4;
+    if (a.dtype == KEEP_F32)
+      *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + o_at) = o;
+    else
+      *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + o_at) =
+          make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]));
+    if (d4 == 0 && a.lse)
+      a.lse[(int64_t)(q.row0 + token) * a.n_q_heads + head] = 0.6931471805599453f * (m + log2f(l));
+  }
+}
+
+uint64_t part_bytes(int tr, int dh) { return (uint64_t)2 * PAGED_WORKERS * tr * (dh + 2) * sizeof(float); }
+constexpr uint64_t REC_BYTES = (PAGED_WORKERS * sizeof(PagedRecord) + 255) & ~(uint64_t)255;
+
+}  // namespace
+
+void launch_paged_generic(const PagedArgs& a, hipStream_t s) {
+  const int dh = a.c.head_dim;
+  // tiles (or the waves' outputs, which need no more) and statistics; the division of the work before that
+  const size_t lds = std::max<size_t>(((size_t)2 * GT_KEYS * (dh + 4) + 128) * sizeof(float), (size_t)8 * (a.n_seqs + 260));
+  const auto kernel = dh <= 64 ? k_paged_generic<4> : dh <= 128 ? k_paged_generic<8> : k_paged_generic<16>;
+  static std::atomic<uint64_t> done[3];
+  set_max_dyn_smem_once(done[dh <= 64 ? 0 : dh <= 128 ? 1 : 2], reinterpret_cast<const void*>(kernel), 150 * 1024);
+  hipLaunchKernelGGL(kernel, dim3(PAGED_WORKERS), dim3(256), lds, s, a);
+  hipLaunchKernelGGL(k_paged_join<GT_ROWS>, dim3(PAGED_WORKERS, 4), dim3(256), 0, s, a);
+}
+
+}  // namespace keep
+
+using namespace keep;
+
+extern "C" uint64_t keep_paged_attention_workspace_bytes(const keep_paged_cache* cache, int32_t n_q_heads, int32_t n_seqs) {
+  if (check_cache(cache, "keep_paged_attention_workspace_bytes") != KEEP_OK) return 0;
+  if (n_q_heads < 1 || n_q_heads % cache->n_kv_heads || n_seqs < 0 || n_seqs > KEEP_PAGED_MAX_SEQS) return 0;
+  return REC_BYTES + part_bytes(GT_ROWS, cache->head_dim);
+}
+
+extern "C" keep_status keep_paged_attention(const keep_paged_attention_desc* d, const keep_paged_cache* cache, const void* q,
+                                            const int32_t* q_start, const int32_t* kv_len, const int32_t* page_table, void* out,
+                                            float* lse, void* workspace, uint64_t workspace_bytes, void* stream) {
+  const char* me = "keep_paged_attention";
+  if (!d) return serve_fail(KEEP_ERR_INVALID_ARG, "%s: desc is NULL", me);
+  const keep_status st = check_cache(cache, me);
+  if (st != KEEP_OK) return st;
+  if (!is_dtype(d->dtype)) return serve_fail(KEEP_ERR_INVALID_ARG, "%s: unknown dtype %d", me, d->dtype);
+  if (d->n_seqs < 0 || d->n_rows < 0 || d->window < 0)
+    return serve_fail(KEEP_ERR_INVALID_ARG, "%s: n_seqs, n_rows or window is negative", me);
+  if (d->n_seqs > KEEP_PAGED_MAX_SEQS)
+    return serve_fail(KEEP_ERR_SHAPE, "%s: more than %d sequences", me, KEEP_PAGED_MAX_SEQS);
+  if (d->n_q_heads < 1 || d->n_q_heads % cache->n_kv_heads)
+    return serve_fail(KEEP_ERR_INVALID_ARG, "%s: n_q_heads %d is no multiple of n_kv_heads %d", me, d->n_q_heads,
+                      cache->n_kv_heads);
+  if (d->max_pages < 1 || (int64_t)d->max_pages * cache->page_size > INT32_MAX - 1023)
+    return serve_fail(KEEP_ERR_INVALID_ARG, "%s: max_pages must be at least 1 and max_pages * page_size at most 2^31 - 1024", me);
+  if (!isfinite(d->scale)) return serve_fail(KEEP_ERR_INVALID_ARG, "%s: scale is not finite", me);
+  const int size = dtype_size(d->dtype);
+  const int64_t width = (int64_t)d->n_q_heads * cache->head_dim;
+  if (d->n_rows * (int64_t)(d->n_q_heads / cache->n_kv_heads) > INT32_MAX - 1024)
+    return serve_fail(KEEP_ERR_SHAPE, "%s: too many query rows", me);
+  if (d->q_stride < width || d->out_stride < width || d->q_stride * size % 16 || d->out_stride * size % 16)
+    return serve_fail(KEEP_ERR_INVALID_ARG, "%s: a row stride must hold the row's %lld values and be a multiple of 16 bytes", me,
+                      (long long)width);
+  if (d->n_seqs == 0 || d->n_rows == 0) return KEEP_OK;
+  if (!q || !q_start || !kv_len || !page_table || !out || !workspace)
+    return serve_fail(KEEP_ERR_INVALID_ARG, "%s: q / q_start / kv_len / page_table / out / workspace is NULL", me);
+  if (!aligned16(q) || !aligned16(out) || reinterpret_cast<uintptr_t>(workspace) % 256)
+    return serve_fail(KEEP_ERR_INVALID_ARG, "%s: q, out or workspace is not aligned", me);
+  if (overlaps(q, row_span(d->n_rows, d->q_stride, width, size), out, row_span(d->n_rows, d->out_stride, width, size)))
+    return serve_fail(KEEP_ERR_INVALID_ARG, "%s: q and out overlap", me);
+  if (workspace_bytes < keep_paged_attention_workspace_bytes(cache, d->n_q_heads, d->n_seqs))
+    return serve_fail(KEEP_ERR_WORKSPACE, "%s: workspace of %llu bytes is too small", me, (unsigned long long)workspace_bytes);
+  PagedArgs a{};
+  a.c = *cache;
+  a.q = q;
+  a.out = out;
+  a.lse = lse;
+  a.q_start = q_start;
+  a.kv_len = kv_len;
+  a.table = page_table;
+  a.q_stride = d->q_stride;
+  a.out_stride = d->out_stride;
+  a.n_seqs = d->n_seqs;
+  a.n_rows = d->n_rows;
+  a.n_q_heads = d->n_q_heads;
+  a.rep = d->n_q_heads / cache->n_kv_heads;
+  a.max_pages = d->max_pages;
+  a.window = d->window;
+  a.capacity = d->max_pages * cache->page_size;
+  a.dtype = d->dtype;
+  a.scale_log2e = (d->scale == 0.f ? 1.f / sqrtf((float)cache->head_dim) : d->scale) * 1.4426950408889634f;
+  a.by_page = fast_div((uint32_t)cache->page_size);
+  a.by_rep = fast_div((uint32_t)a.rep);
+  char* ws = static_cast<char*>(workspace);
+  a.rec = reinterpret_cast<PagedRecord*>(ws);
+  a.part_ml = reinterpret_cast<float*>(ws + REC_BYTES);
+  a.part_o = a.part_ml + (size_t)2 * PAGED_WORKERS * 2 * GT_ROWS;
+  if (!format_scaled(cache->format)) a.c.k_scale = a.c.v_scale = nullptr;
+  launch_paged_generic(a, static_cast<hipStream_t>(stream));
+  return launched(me);
+}
