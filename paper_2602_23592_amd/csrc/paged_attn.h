@@ -49,6 +49,15 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedArgs& a, int s) {
   return q;
 }
 
+// The same number in every lane, kept in a scalar register so that what depends on it branches and loads as one
+__device__ __forceinline__ int paged_uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ uint64_t paged_uniform(uint64_t v) {
+  return (uint64_t)(uint32_t)paged_uniform((int)(v >> 32)) << 32 | (uint32_t)paged_uniform((int)v);
+}
+__device__ __forceinline__ PagedSeq paged_uniform(PagedSeq q) {
+  return PagedSeq{paged_uniform(q.row0), paged_uniform(q.rows), paged_uniform(q.len)};
+}
+
 // Key tiles of one tile of query rows: [first, first + units)
 template <int TR, int KT>
 __device__ __forceinline__ void paged_span(const PagedArgs& a, const PagedSeq& q, int tile, int& first, int& units) {
@@ -164,7 +173,8 @@ __device__ __forceinline__ PagedPlace paged_place(const PagedArgs& a, int worker
       at -= __shfl((unsigned long long)sum, 63, 64);
     }
   }
-  return p;
+  return PagedPlace{paged_uniform(p.total), paged_uniform(p.begin), paged_uniform(p.end),  paged_uniform(p.seq),
+                    paged_uniform(p.head),  paged_uniform(p.tile),  paged_uniform(p.unit)};
 }
 
 // The job behind (seq, head, tile); sequences without rows are passed over.  Only called where another job exists.
@@ -175,7 +185,7 @@ __device__ __forceinline__ void paged_next(const PagedArgs& a, PagedPlace& p, Pa
   p.tile = 0;
   if (++p.head < a.c.n_kv_heads) return;
   p.head = 0;
-  do q = paged_seq(a, ++p.seq);
+  do q = paged_uniform(paged_seq(a, ++p.seq));
   while (q.rows == 0 && p.seq + 1 < a.n_seqs);
 }
 
@@ -187,6 +197,60 @@ __device__ __forceinline__ int64_t paged_key(const PagedArgs& a, const int32_t* 
   return page * a.c.page_stride + at * a.c.token_stride;
 }
 
+typedef __attribute__((ext_vector_type(4))) float paged_f32x4;
+
+// The four waves' parts of a job (each of other keys), added in their order: the job's result, or a partial one where the job
+// was cut.  so: LDS [4 waves][head_dim / 4][TR][4]; sml: LDS [2][4 waves][TR], maxima and sums.
+template <int TR>
+__device__ __forceinline__ void paged_finish(const PagedArgs& a, const PagedPlace& p, const PagedSeq& q, int worker, uint64_t at,
+                                             int u0, int u1, int units, const float* so, const float* sml) {
+  const int tid = threadIdx.x, row = tid % TR, quads = a.c.head_dim / 4;
+  const int x = p.tile * TR + row;
+  const bool valid = x < q.rows * a.rep, whole = u0 == 0 && u1 == units;
+  const int token = valid ? (int)div_by(x, a.by_rep) : 0, head = p.head * a.rep + (valid ? x - token * a.rep : 0);
+  const int64_t slot = 2 * worker + (u0 == 0 ? 1 : 0);
+  float mw[4], m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) m = fmaxf(m, mw[w] = sml[w * TR + row]);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    mw[w] = mw[w] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw[w] - m);
+    l += sml[(4 + w) * TR + row] * mw[w];
+  }
+  for (int d4 = tid / TR; d4 < quads; d4 += 256 / TR) {
+    paged_f32x4 o{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const paged_f32x4 v = *reinterpret_cast<const paged_f32x4*>(so + ((w * quads + d4) * TR + row) * 4);
+      o += mw[w] == 0.f ? paged_f32x4{0.f, 0.f, 0.f, 0.f} : v * mw[w];
+    }
+    if (!whole) {
+      *reinterpret_cast<paged_f32x4*>(a.part_o + ((slot * quads + d4) * TR + row) * 4) = o;
+    } else if (valid) {
+      if (l != 0.f) o /= l;
+      const int64_t o_at = (int64_t)(q.row0 + token) * a.out_stride + (int64_t)head * a.c.head_dim + d4 * 4;
+      if (a.dtype == KEEP_F32)
+        *reinterpret_cast<paged_f32x4*>(static_cast<float*>(a.out) + o_at) = o;
+      else
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + o_at) =
+            make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]));
+    }
+  }
+  if (tid < TR) {
+    if (!whole) {
+      a.part_ml[slot * 2 * TR + row] = m;
+      a.part_ml[(slot * 2 + 1) * TR + row] = l;
+    } else if (valid && a.lse) {
+      a.lse[(int64_t)(q.row0 + token) * a.n_q_heads + head] = 0.6931471805599453f * (m + log2f(l));
+    }
+  }
+  if (tid == 0 && u0 == 0 && !whole)
+    a.rec[worker] = PagedRecord{p.seq, p.head, p.tile, paged_worker_of(at + units - 1, p.total)};
+}
+
 void launch_paged_generic(const PagedArgs& a, hipStream_t s);
+// bf16 queries, heads of 64 or 128, a bf16 or 8-bit cache of less than 64 GB per tensor; rows: query rows of a tile (16 or 32)
+void launch_paged_few(const PagedArgs& a, int rows, hipStream_t s);
+void launch_paged_join(const PagedArgs& a, int rows, hipStream_t s);
 
 }  // namespace keep

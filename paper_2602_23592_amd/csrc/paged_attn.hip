@@ -10,7 +10,7 @@
 namespace keep {
 namespace {
 
-typedef __attribute__((ext_vector_type(4))) float f32x4;
+using f32x4 = paged_f32x4;
 
 constexpr int GT_ROWS = 16, GT_KEYS = 64;
 
@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(256) k_paged_generic(PagedArgs a) {
   float* sk = lds;
   float* sv = lds + GT_KEYS * stride;
   float* sml = sv + GT_KEYS * stride;  // [2][4 waves][16]
-  PagedSeq q = paged_seq(a, p.seq);
+  PagedSeq q = paged_uniform(paged_seq(a, p.seq));
   for (uint64_t at = p.begin;;) {
     int first, units;
     paged_span<GT_ROWS, GT_KEYS>(a, q, p.tile, first, units);
@@ -171,48 +171,7 @@ __global__ void __launch_bounds__(256) k_paged_generic(PagedArgs a) {
     for (int i = 0; i < ND; ++i)
       if (i < nd) *reinterpret_cast<f32x4*>(so + ((wave * (dh / 4) + 4 * i + g) * 16 + col) * 4) = acc[i];
     __syncthreads();
-    const bool whole = u0 == 0 && u1 == units;
-    const int slot = 2 * worker + (u0 == 0 ? 1 : 0);
-    {
-      float mw[4], m_all = -INFINITY, l_all = 0.f;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) m_all = fmaxf(m_all, mw[w] = sml[w * 16 + col]);
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        mw[w] = mw[w] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw[w] - m_all);
-        l_all += sml[64 + w * 16 + col] * mw[w];
-      }
-      // (a thread keeps the query row of its lane: tid % 16 = col)
-      for (int d4 = tid >> 4; d4 < dh / 4; d4 += 16) {
-        f32x4 o{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const f32x4 v = *reinterpret_cast<const f32x4*>(so + ((w * (dh / 4) + d4) * 16 + col) * 4);
-          o += mw[w] == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : v * mw[w];
-        }
-        if (!whole) {
-          *reinterpret_cast<f32x4*>(a.part_o + (((int64_t)slot * (dh / 4) + d4) * GT_ROWS + col) * 4) = o;
-        } else if (valid) {
-          if (l_all != 0.f) o /= l_all;
-          const int64_t o_at = (int64_t)(q.row0 + token) * a.out_stride + (int64_t)head * dh + d4 * 4;
-          if (a.dtype == KEEP_F32)
-            *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + o_at) = o;
-          else
-            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + o_at) =
-                make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]));
-        }
-      }
-      if (tid < 16) {
-        if (!whole) {
-          a.part_ml[(slot * 2) * GT_ROWS + col] = m_all;
-          a.part_ml[(slot * 2 + 1) * GT_ROWS + col] = l_all;
-        } else if (valid && a.lse) {
-          a.lse[(int64_t)(q.row0 + token) * a.n_q_heads + head] = 0.6931471805599453f * (m_all + log2f(l_all));
-        }
-      }
-    }
-    if (tid == 0 && u0 == 0 && !whole)
-      a.rec[worker] = PagedRecord{p.seq, p.head, p.tile, paged_worker_of(at + units - 1, p.total)};
+    paged_finish<GT_ROWS>(a, p, q, worker, at, u0, u1, units, so, sml);
     at += u1 - u0;
     if (at >= p.end) break;
     paged_next<GT_ROWS>(a, p, q);
@@ -282,7 +241,12 @@ void launch_paged_generic(const PagedArgs& a, hipStream_t s) {
   static std::atomic<uint64_t> done[3];
   set_max_dyn_smem_once(done[dh <= 64 ? 0 : dh <= 128 ? 1 : 2], reinterpret_cast<const void*>(kernel), 150 * 1024);
   hipLaunchKernelGGL(kernel, dim3(PAGED_WORKERS), dim3(256), lds, s, a);
-  hipLaunchKernelGGL(k_paged_join<GT_ROWS>, dim3(PAGED_WORKERS, 4), dim3(256), 0, s, a);
+  launch_paged_join(a, GT_ROWS, s);
+}
+
+void launch_paged_join(const PagedArgs& a, int rows, hipStream_t s) {
+  const auto kernel = rows == 16 ? k_paged_join<16> : k_paged_join<32>;
+  hipLaunchKernelGGL(kernel, dim3(PAGED_WORKERS, 4), dim3(256), 0, s, a);
 }
 
 }  // namespace keep
@@ -292,7 +256,7 @@ using namespace keep;
 extern "C" uint64_t keep_paged_attention_workspace_bytes(const keep_paged_cache* cache, int32_t n_q_heads, int32_t n_seqs) {
   if (check_cache(cache, "keep_paged_attention_workspace_bytes") != KEEP_OK) return 0;
   if (n_q_heads < 1 || n_q_heads % cache->n_kv_heads || n_seqs < 0 || n_seqs > KEEP_PAGED_MAX_SEQS) return 0;
-  return REC_BYTES + part_bytes(GT_ROWS, cache->head_dim);
+  return REC_BYTES + part_bytes(32, cache->head_dim);
 }
 
 extern "C" keep_status keep_paged_attention(const keep_paged_attention_desc* d, const keep_paged_cache* cache, const void* q,
@@ -353,8 +317,18 @@ extern "C" keep_status keep_paged_attention(const keep_paged_attention_desc* d, 
   char* ws = static_cast<char*>(workspace);
   a.rec = reinterpret_cast<PagedRecord*>(ws);
   a.part_ml = reinterpret_cast<float*>(ws + REC_BYTES);
-  a.part_o = a.part_ml + (size_t)2 * PAGED_WORKERS * 2 * GT_ROWS;
   if (!format_scaled(cache->format)) a.c.k_scale = a.c.v_scale = nullptr;
-  launch_paged_generic(a, static_cast<hipStream_t>(stream));
+  // The bf16 matrix instruction where it has a kernel.  Tiles of 16 query rows while sequences bring no more on average
+  // (one to a few tokens), else of 32.
+  const int64_t span = (int64_t)(cache->n_pages - 1) * cache->page_stride + (int64_t)(cache->n_kv_heads - 1) * cache->head_stride +
+                       (int64_t)(cache->page_size - 1) * cache->token_stride + cache->head_dim;
+  const bool mfma = d->dtype == KEEP_BF16 && cache->format != KEEP_CACHE_F32 &&
+                    (cache->head_dim == 64 || cache->head_dim == 128) && span * format_size(cache->format) < (int64_t)64 << 30;
+  const int rows = !mfma || d->n_rows * (int64_t)a.rep <= 16 * (int64_t)d->n_seqs ? 16 : 32;
+  a.part_o = a.part_ml + (size_t)2 * PAGED_WORKERS * 2 * rows;
+  if (mfma)
+    launch_paged_few(a, rows, static_cast<hipStream_t>(stream));
+  else
+    launch_paged_generic(a, static_cast<hipStream_t>(stream));
   return launched(me);
 }

@@ -1,0 +1,438 @@
+// Attention over pages on the bf16 matrix instruction: bf16 queries, heads of 64 or 128, a bf16 or 8-bit cache.
+//
+// k_paged_few: tiles of 16 or 32 query rows (one to a few tokens with their heads), where the keys are read once for few rows and
+// memory is the bound.  Each of a workgroup's four waves streams key slices of its own (32 of a unit's 128 keys) through its own
+// part of LDS, without barriers: K and V arrive by loads that go straight to LDS as they are stored, the next slice's K is
+// requested as soon as this one's has been read and the same for V, so that a wave always has loads in flight; two workgroups
+// per CU keep some 100 KB on their way.
+//
+// Scores are formed transposed, S^T = K . Q^T (16x16x32): a lane owns a query row (lane % 16) and keys 4 (lane / 16) + r of both
+// 16-key blocks, which as they stand are the operand of O^T = V^T . P^T; its V^T operand comes from the transposing LDS
+// reads (ds_read_b64_tr_b16, _tr_b8).  8-bit codes become bf16 exactly (at most 8 significant bits) when they are read as
+// operands; a key's scale multiplies its scores, a value's scale its probability, in binary32.  Probabilities (with the
+// value's scale) are rounded to bf16 for the product, the row sums are taken before that.
+#include "paged_attn.h"
+
+namespace keep {
+namespace {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((ext_vector_type(2))) int i32x2;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+using f32x4 = paged_f32x4;
+typedef s16x4 __attribute__((address_space(3))) * lds_s16x4;
+typedef i32x2 __attribute__((address_space(3))) * lds_i32x2;
+typedef char __attribute__((address_space(3))) * lds_char;
+
+__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(lds_char)p; }
+
+// 16 (4) bytes per lane from global memory to LDS address `to` + 16 (4) * lane.  Written out because the compiler would wait
+// for these loads before every later LDS read; vm_wait below says which have landed.  (m0 holds the LDS address; nothing that
+// the compiler makes of these kernels reads it.)
+__device__ __forceinline__ void load_lds16(const void* from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
+}
+__device__ __forceinline__ void load_lds4(const void* from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(to) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void vm_wait() {  // all but the N youngest vector loads have landed
+  static_assert(N >= 0 && N < 64, "the counter has six bits");
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void lds_wait() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// Over the four lanes of a query row (lane % 16)
+__device__ __forceinline__ float row_max(float v) {
+  auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float row_sum(float v) {
+  v += __shfl_xor(v, 16, 64);
+  return v + __shfl_xor(v, 32, 64);
+}
+
+// Eight codes as bf16 numbers
+template <int FMT>
+__device__ __forceinline__ bf16x8 codes8(uint32_t lo, uint32_t hi) {
+  u32x4 r;
+  if constexpr (FMT == KEEP_CACHE_FP8) {
+    r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false));
+    r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true));
+    r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false));
+    r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t w = i ? hi : lo;
+      r[2 * i] = pack_bf16x2((float)(int8_t)w, (float)(int8_t)(w >> 8));
+      r[2 * i + 1] = pack_bf16x2((float)(int8_t)(w >> 16), (float)(int8_t)(w >> 24));
+    }
+  }
+  return __builtin_bit_cast(bf16x8, r);
+}
+
+// Where the 16-byte chunk c of a slice's row lies inside the row.  LDS serves 256 bytes at a time: a K read 16 rows (lane % 16) at one
+// chunk, a V read half a wave: eight rows of two chunks (bf16), or 16 rows (4 g + j and 16 + 4 g + j, two g) of one chunk.
+// CH: chunks per row; 16 / CH rows share a stretch of 256 bytes, the chunks of those that lie at the same place move apart.
+template <int CH>
+__device__ __forceinline__ int k_chunk(int row, int c) {
+  return CH == 16 ? c ^ (row & 15) : CH == 8 ? c ^ ((row >> 1) & 7) : c ^ ((row >> 2) & 3);
+}
+template <int CH, bool WIDE>  // WIDE: bf16
+__device__ __forceinline__ int v_chunk(int row, int c) {
+  if (WIDE) return CH == 16 ? c ^ (2 * (row & 7)) : c ^ (2 * ((row >> 1) & 3));
+  return CH == 8 ? c ^ (((row >> 1) & 3) | ((row >> 2) & 4)) : c ^ (((row >> 2) & 1) | ((row >> 3) & 2));
+}
+
+constexpr int SLICE = 32, UNIT = 4 * SLICE;  // keys of a wave's slice, of a unit
+constexpr int TABLE = 1024;                  // page table entries held in LDS at a time
+
+template <int DH, int FMT, int RB>
+struct Few {
+  static constexpr bool WIDE = FMT == KEEP_CACHE_BF16;
+  static constexpr int TR = 16 * RB;
+  static constexpr int ROW = DH * (WIDE ? 2 : 1), CH = ROW / 16;  // bytes and chunks of a key
+  static constexpr int PER = 64 / CH, NI = SLICE / PER;           // rows of a load, loads of a slice
+  static constexpr int BYTES = SLICE * ROW;
+  static constexpr int NS = 16384 / (2 * BYTES);                  // slices in flight
+  static constexpr int NK = NI + (WIDE ? 0 : 1), NV = NI;         // loads of a slice's K (with the scales) and V
+  static constexpr int WAVE = NS * (2 * BYTES + (WIDE ? 0 : 256));
+  static constexpr int ML = 4 * WAVE, TBL = ML + 8 * TR * 4, LDS = TBL + TABLE * 4;
+  static_assert(4 * TR * DH * 4 <= 4 * WAVE, "the waves' outputs lie where the slices did");
+};
+
+template <int DH, int FMT, int RB>
+__global__ void __launch_bounds__(256, 2) k_paged_few(PagedArgs a) {
+  using F = Few<DH, FMT, RB>;
+  constexpr int TR = F::TR, ROW = F::ROW, CH = F::CH, NS = F::NS, DT = DH / 16, KS = DH / 32;
+  extern __shared__ __attribute__((aligned(256))) char lds[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, g = lane >> 4;
+  // The workgroups of an XCD (blockIdx % 8) take neighbouring runs: one head's tiles read the same keys from its L2
+  const int worker = (blockIdx.x & 7) * (PAGED_WORKERS / 8) + (blockIdx.x >> 3);
+  PagedPlace p = paged_place<TR, UNIT>(a, worker, reinterpret_cast<uint64_t*>(lds));
+  if (tid == 0) a.rec[worker].last = 0;
+  if (p.begin >= p.end) return;
+  char* ring = lds + wave * F::WAVE;  // [NS] K slices, [NS] V slices, [NS] scales (32 of keys, 32 of values)
+  const uint32_t ring_at = __builtin_amdgcn_readfirstlane(lds_address(ring));
+  float* sml = reinterpret_cast<float*>(lds + F::ML);
+  int32_t* tbl = reinterpret_cast<int32_t*>(lds + F::TBL);
+  const char* k_base = static_cast<const char*>(a.c.k);
+  const char* v_base = static_cast<const char*>(a.c.v);
+  const int block_units = (int)max((int64_t)1, min((int64_t)1 << 20, (int64_t)(TABLE - 2) * a.c.page_size / UNIT));
+  PagedSeq q = paged_uniform(paged_seq(a, p.seq));
+
+  for (uint64_t at = p.begin;;) {
+    int first, units;
+    paged_span<TR, UNIT>(a, q, p.tile, first, units);
+    const int u0 = p.unit, u1 = (int)min((uint64_t)units, u0 + (p.end - at));
+    // ---- this lane's query rows
+    int pos[RB], lo[RB];
+    bf16x8 qf[RB][KS];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+      const int x = p.tile * TR + b * 16 + col;
+      const bool valid = x < q.rows * a.rep;
+      const int token = valid ? (int)div_by(x, a.by_rep) : 0;
+      pos[b] = valid ? q.len - q.rows + token : -1;
+      lo[b] = a.window ? max(0, pos[b] - a.window + 1) : 0;
+      const __bf16* qp = static_cast<const __bf16*>(a.q) + (int64_t)(q.row0 + token) * a.q_stride +
+                         (int64_t)(p.head * a.rep + (valid ? x - token * a.rep : 0)) * DH;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)  // the dimensions that the K operand of step ks holds
+        qf[b][ks] = *reinterpret_cast<const bf16x8*>(qp + (F::WIDE ? ks * 32 + g * 8 : (ks >> 1) * 64 + g * 16 + (ks & 1) * 8));
+    }
+    // (the queries are in registers before the slices' loads begin: the compiler would wait for them, and so for those, in
+    // every slice)
+#pragma unroll
+    for (int b = 0; b < RB; ++b)
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[b][ks]));
+    int max_pos, min_pos, max_lo;  // over the tile
+    {
+      const int x1 = min(q.rows * a.rep, (p.tile + 1) * TR) - 1;
+      max_pos = q.len - q.rows + (int)div_by(x1, a.by_rep);
+      min_pos = q.len - q.rows + (int)div_by(p.tile * TR, a.by_rep);
+      max_lo = a.window ? max(0, max_pos - a.window + 1) : 0;
+    }
+    f32x4 acc[RB][DT];
+    float m[RB], l[RB];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+      m[b] = -INFINITY, l[b] = 0.f;
+#pragma unroll
+      for (int i = 0; i < DT; ++i) acc[b][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const int32_t* table = a.table + (int64_t)p.seq * a.max_pages;
+    const int64_t head_at = (int64_t)p.head * a.c.head_stride * (F::WIDE ? 2 : 1);
+
+    for (int ub = u0; ub < u1; ub += block_units) {
+      const int ue = min(u1, ub + block_units);
+      const int page0 = (int)div_by((uint32_t)(first + ub) * UNIT, a.by_page);
+      const int page1 = (int)div_by((uint32_t)min((int64_t)(first + ue) * UNIT - 1, (int64_t)max(q.len, 1) - 1), a.by_page);
+      __syncthreads();  // earlier entries, or the outputs of the job before, have been read
+      for (int i = tid; i <= page1 - page0; i += 256) tbl[i] = min(max(table[page0 + i], 0), a.c.n_pages - 1);
+      __syncthreads();
+      // ---- this wave's slices: keys key0 + UNIT * t, while some row sees them
+      const int key0 = (first + ub) * UNIT + wave * SLICE;
+      const int n = key0 > max_pos ? 0 : min(ue - ub, (max_pos - key0) / UNIT + 1);
+      uint32_t v_off = 0;  // per lane: where key lane % 32 of the youngest requested slice lies, in 16 bytes
+      const auto request_k = [&](int t) {
+        const int key = min(key0 + t * UNIT + (lane & 31), q.len - 1), pg = (int)div_by(key, a.by_page);
+        const int page = tbl[pg - page0], in = key - pg * a.c.page_size;
+        const uint32_t off = (uint32_t)((page * a.c.page_stride + in * a.c.token_stride) * (F::WIDE ? 2 : 1) / 16);
+        const int slot = t % NS;
+        if constexpr (!F::WIDE)
+          load_lds4((lane < 32 ? a.c.k_scale : a.c.v_scale) + ((int64_t)page * a.c.n_kv_heads + p.head) * a.c.page_size + in,
+                    ring_at + 2 * NS * F::BYTES + slot * 256);
+#pragma unroll
+        for (int i = 0; i < F::NI; ++i) {
+          const int row = i * F::PER + lane / CH;
+          load_lds16(k_base + head_at + (int64_t)(uint32_t)__shfl((int)off, row, 64) * 16 + k_chunk<CH>(row, lane % CH) * 16,
+                     ring_at + slot * F::BYTES + i * 1024);
+        }
+        return off;
+      };
+      const auto request_v = [&](int t) {
+        const int slot = t % NS;
+#pragma unroll
+        for (int i = 0; i < F::NI; ++i) {
+          const int row = i * F::PER + lane / CH;
+          load_lds16(v_base + head_at + (int64_t)(uint32_t)__shfl((int)v_off, row, 64) * 16 + v_chunk<CH, F::WIDE>(row, lane % CH) * 16,
+                     ring_at + (NS + slot) * F::BYTES + i * 1024);
+        }
+      };
+      if (n > 0) vm_wait<0>();  // (nothing of the compiler's own is counted below)
+      for (int t = 0; t < min(n, NS); ++t) {
+        v_off = request_k(t);
+        request_v(t);
+      }
+      for (int t = 0; t < n; ++t) {
+        const int slot = t % NS, kb = key0 + t * UNIT, left = min(NS - 1, n - 1 - t);
+        const char* sk = ring + slot * F::BYTES;
+        const char* sv = ring + (NS + slot) * F::BYTES;
+        const float* scales = reinterpret_cast<const float*>(ring + 2 * NS * F::BYTES + slot * 256);
+        // K of this slice has landed; behind it V and `left` whole slices were requested
+        switch (left) {
+          case 0: vm_wait<F::NV>(); break;
+          case 1: vm_wait<F::NV + F::NK + F::NV>(); break;
+          case 2: vm_wait<F::NV + 2 * (F::NK + F::NV)>(); break;
+          default: vm_wait<F::NV + 3 * (F::NK + F::NV)>(); break;
+        }
+        f32x4 s[RB][2];
+#pragma unroll
+        for (int b = 0; b < RB; ++b) s[b][0] = s[b][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kb16 = 0; kb16 < 2; ++kb16) {
+          const int row = kb16 * 16 + col;
+          if constexpr (F::WIDE) {
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+              const bf16x8 kf = *reinterpret_cast<const bf16x8*>(sk + row * ROW + k_chunk<CH>(row, 4 * ks + g) * 16);
+#pragma unroll
+              for (int b = 0; b < RB; ++b) s[b][kb16] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[b][ks], s[b][kb16], 0, 0, 0);
+            }
+          } else {
+#pragma unroll
+            for (int k2 = 0; k2 < KS / 2; ++k2) {
+              const u32x4 c = *reinterpret_cast<const u32x4*>(sk + row * ROW + k_chunk<CH>(row, 4 * k2 + g) * 16);
+              const bf16x8 f0 = codes8<FMT>(c[0], c[1]), f1 = codes8<FMT>(c[2], c[3]);
+#pragma unroll
+              for (int b = 0; b < RB; ++b) {
+                s[b][kb16] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f0, qf[b][2 * k2], s[b][kb16], 0, 0, 0);
+                s[b][kb16] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f1, qf[b][2 * k2 + 1], s[b][kb16], 0, 0, 0);
+              }
+            }
+          }
+        }
+        f32x4 k_sc[2], v_sc[2];
+        if constexpr (!F::WIDE) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            k_sc[i] = *reinterpret_cast<const f32x4*>(scales + i * 16 + 4 * g) * a.scale_log2e;
+            v_sc[i] = *reinterpret_cast<const f32x4*>(scales + 32 + i * 16 + 4 * g);
+          }
+        }
+        lds_wait();  // K and the scales are in registers: their places may be written
+        if (t + NS < n) v_off = request_k(t + NS);
+
+        // ---- scores in the log2 domain, running maximum and sum
+        const bool masked = kb + SLICE - 1 > min_pos || kb < max_lo;
+        bf16x8 pf[RB];
+        float pr[RB][8];
+#pragma unroll
+        for (int b = 0; b < RB; ++b) {
+          float top = -INFINITY;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            float v = s[b][e >> 2][e & 3];
+            if constexpr (F::WIDE)
+              v *= a.scale_log2e;
+            else
+              v *= k_sc[e >> 2][e & 3];
+            if (masked) {
+              const int key = kb + (e >> 2) * 16 + 4 * g + (e & 3);
+              v = key <= pos[b] && key >= lo[b] ? v : -INFINITY;
+            }
+            pr[b][e] = v;
+            top = fmaxf(top, v);
+          }
+          const float m_new = fmaxf(m[b], row_max(top)), m_ref = m_new == -INFINITY ? 0.f : m_new;
+          if (__ballot(m_new != m[b])) {
+            const float alpha = __builtin_amdgcn_exp2f(m[b] - m_ref);
+            l[b] *= alpha;
+#pragma unroll
+            for (int i = 0; i < DT; ++i) acc[b][i] *= alpha;
+            m[b] = m_new;
+          }
+          u32x4 pk;
+#pragma unroll
+          for (int e = 0; e < 8; e += 2) {
+            float p0 = __builtin_amdgcn_exp2f(pr[b][e] - m_ref), p1 = __builtin_amdgcn_exp2f(pr[b][e + 1] - m_ref);
+            l[b] += p0 + p1;
+            if constexpr (!F::WIDE) {
+              const float v0 = v_sc[e >> 2][e & 3], v1 = v_sc[e >> 2][(e & 3) + 1];
+              // (a scale of NaN must not reach rows that do not see the key)
+              p0 = masked && pr[b][e] == -INFINITY ? 0.f : p0 * v0;
+              p1 = masked && pr[b][e + 1] == -INFINITY ? 0.f : p1 * v1;
+            }
+            pr[b][e] = p0, pr[b][e + 1] = p1;
+            pk[e >> 1] = pack_bf16x2(p0, p1);
+          }
+          pf[b] = __builtin_bit_cast(bf16x8, pk);
+        }
+
+        // ---- V of this slice has landed; behind it the K requested above and `left` slices of before
+        if (t + NS < n) {
+          vm_wait<(NS - 1) * (F::NK + F::NV) + F::NK>();
+        } else {
+          switch (left) {
+            case 0: vm_wait<0>(); break;
+            case 1: vm_wait<F::NK + F::NV>(); break;
+            case 2: vm_wait<2 * (F::NK + F::NV)>(); break;
+            default: vm_wait<3 * (F::NK + F::NV)>(); break;
+          }
+        }
+        bool odd = false;
+        if (masked && FMT != KEEP_CACHE_INT8) {
+          // A product with a probability of zero would carry infinities and NaN to rows that do not see the key.
+          constexpr uint32_t EXP = F::WIDE ? 0x7f807f80u : 0x7f7f7f7fu;
+          for (int i = lane; i < F::BYTES / 16; i += 64) {
+            const u32x4 w = *reinterpret_cast<const u32x4*>(sv + i * 16);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t x = (w[e] & EXP) ^ EXP;  // a field of zeros: infinity or NaN
+              odd = odd || (F::WIDE ? !(x & 0xffffu) || !(x >> 16)
+                                    : !(x & 0xffu) || !(x & 0xff00u) || !(x & 0xff0000u) || !(x >> 24));
+            }
+          }
+          odd = __ballot(odd) != 0;
+        }
+        if (!odd) {
+#pragma unroll
+          for (int i = 0; i < DT; ++i) {
+            bf16x8 vf;
+            if constexpr (F::WIDE) {
+              const int row = 4 * g + (col >> 2), in = 8 * (col & 1), c = 2 * i + ((col & 3) >> 1);
+              const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(sv + row * ROW + v_chunk<CH, true>(row, c) * 16 + in));
+              const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                  (lds_s16x4)(sv + (row + 16) * ROW + v_chunk<CH, true>(row + 16, c) * 16 + in));
+              vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+            } else {
+              const int j = col >> 1, row = 4 * g + (j & 3) + 4 * (j & 4);
+              const i32x2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                  (lds_i32x2)(sv + row * ROW + v_chunk<CH, false>(row, i) * 16 + 8 * (col & 1)));
+              vf = codes8<FMT>((uint32_t)v[0], (uint32_t)v[1]);
+            }
+#pragma unroll
+            for (int b = 0; b < RB; ++b) acc[b][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[b], acc[b][i], 0, 0, 0);
+          }
+        } else {
+#pragma unroll 1
+          for (int j = 0; j < SLICE; ++j) {  // a key at a time, for the rows that see it
+            const int key = kb + j;
+            float pj[RB];
+#pragma unroll
+            for (int b = 0; b < RB; ++b) {  // key j's probability lies in lane 16 (j / 4 % 4) + col, element 4 (j / 16) + j % 4
+              float mine = 0.f;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) mine = (j >> 4) * 4 + (j & 3) == e ? pr[b][e] : mine;
+              pj[b] = __shfl(mine, ((j >> 2) & 3) * 16 + col, 64);
+            }
+#pragma unroll
+            for (int i = 0; i < DT; ++i) {
+              float v[4];  // dimensions 16 i + 4 g + r
+              if constexpr (F::WIDE) {
+                const int d = i * 16 + 4 * g;
+                const uint2 w = *reinterpret_cast<const uint2*>(sv + j * ROW + v_chunk<CH, true>(j, d >> 3) * 16 + (d & 7) * 2);
+                v[0] = bf16_bits_to_f32((uint16_t)w.x), v[1] = bf16_bits_to_f32((uint16_t)(w.x >> 16));
+                v[2] = bf16_bits_to_f32((uint16_t)w.y), v[3] = bf16_bits_to_f32((uint16_t)(w.y >> 16));
+              } else {
+                const int w = *reinterpret_cast<const int*>(sv + j * ROW + v_chunk<CH, false>(j, i) * 16 + 4 * g);
+                const auto v01 = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), v23 = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+                v[0] = v01[0], v[1] = v01[1], v[2] = v23[0], v[3] = v23[1];
+              }
+#pragma unroll
+              for (int b = 0; b < RB; ++b)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[b][i][r] += key <= pos[b] && key >= lo[b] ? pj[b] * v[r] : 0.f;
+            }
+          }
+        }
+        lds_wait();
+        if (t + NS < n) request_v(t + NS);
+      }
+    }
+
+    // ---- the waves' parts to LDS, where the slices were
+#pragma unroll
+    for (int b = 0; b < RB; ++b) l[b] = row_sum(l[b]);
+    __syncthreads();
+    float* so = reinterpret_cast<float*>(lds);
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+      if (g == 0) sml[wave * TR + b * 16 + col] = m[b], sml[(4 + wave) * TR + b * 16 + col] = l[b];
+#pragma unroll
+      for (int i = 0; i < DT; ++i)
+        *reinterpret_cast<f32x4*>(so + ((wave * (DH / 4) + 4 * i + g) * TR + b * 16 + col) * 4) = acc[b][i];
+    }
+    __syncthreads();
+    paged_finish<TR>(a, p, q, worker, at, u0, u1, units, so, sml);
+    at += u1 - u0;
+    if (at >= p.end) break;
+    paged_next<TR>(a, p, q);
+  }
+}
+
+template <int DH, int FMT, int RB>
+void launch_few(const PagedArgs& a, hipStream_t s) {
+  static std::atomic<uint64_t> done{0};
+  const auto kernel = k_paged_few<DH, FMT, RB>;
+  set_max_dyn_smem_once(done, reinterpret_cast<const void*>(kernel), Few<DH, FMT, RB>::LDS);
+  hipLaunchKernelGGL(kernel, dim3(PAGED_WORKERS), dim3(256), (size_t)(Few<DH, FMT, RB>::LDS), s, a);
+}
+template <int DH, int RB>
+void launch_few_format(const PagedArgs& a, hipStream_t s) {
+  if (a.c.format == KEEP_CACHE_BF16)
+    launch_few<DH, KEEP_CACHE_BF16, RB>(a, s);
+  else if (a.c.format == KEEP_CACHE_FP8)
+    launch_few<DH, KEEP_CACHE_FP8, RB>(a, s);
+  else
+    launch_few<DH, KEEP_CACHE_INT8, RB>(a, s);
+}
+
+}  // namespace
+
+void launch_paged_few(const PagedArgs& a, int rows, hipStream_t s) {
+  if (a.c.head_dim == 128)
+    rows == 16 ? launch_few_format<128, 1>(a, s) : launch_few_format<128, 2>(a, s);
+  else
+    rows == 16 ? launch_few_format<64, 1>(a, s) : launch_few_format<64, 2>(a, s);
+  launch_paged_join(a, rows, s);
+}
+
+}  // namespace keep
