@@ -18,8 +18,10 @@ namespace keep {
 constexpr int PAGED_WORKERS = 512;  // two workgroups for each of 256 CUs
 
 struct PagedRecord {  // of a worker: the cut job that begins in it
-  int32_t seq, head, tile;
   int32_t last;       // the last worker of that job; 0: no such job
+  int32_t row0;       // first query row of the sequence
+  int32_t x0, n;      // the tile's query rows: the first (within sequence and head) and their number
+  int32_t head;
 };
 
 struct PagedArgs {
@@ -224,9 +226,10 @@ __device__ __forceinline__ void paged_finish(const PagedArgs& a, const PagedPlac
       const paged_f32x4 v = *reinterpret_cast<const paged_f32x4*>(so + ((w * quads + d4) * TR + row) * 4);
       o += mw[w] == 0.f ? paged_f32x4{0.f, 0.f, 0.f, 0.f} : v * mw[w];
     }
+    if (!valid) continue;
     if (!whole) {
       *reinterpret_cast<paged_f32x4*>(a.part_o + ((slot * quads + d4) * TR + row) * 4) = o;
-    } else if (valid) {
+    } else {
       if (l != 0.f) o /= l;
       const int64_t o_at = (int64_t)(q.row0 + token) * a.out_stride + (int64_t)head * a.c.head_dim + d4 * 4;
       if (a.dtype == KEEP_F32)
@@ -245,7 +248,8 @@ __device__ __forceinline__ void paged_finish(const PagedArgs& a, const PagedPlac
     }
   }
   if (tid == 0 && u0 == 0 && !whole)
-    a.rec[worker] = PagedRecord{p.seq, p.head, p.tile, paged_worker_of(at + units - 1, p.total)};
+    a.rec[worker] = PagedRecord{paged_worker_of(at + units - 1, p.total), q.row0, p.tile * TR, min(TR, q.rows * a.rep - p.tile * TR),
+                                p.head};
 }
 
 void launch_paged_generic(const PagedArgs& a, hipStream_t s);

@@ -179,53 +179,69 @@ __global__ void __launch_bounds__(256) k_paged_generic(PagedArgs a) {
 }
 
 // The parts of a job that was cut, joined in the order of their keys.  A workgroup takes the job that worker blockIdx.x left a
-// record of, and a quarter of the output's dimensions (blockIdx.y).  Threads lie along query rows, then along parts (as
-// many as there are, up to eight and while rows and parts fill a wave: a butterfly adds those), then along dimensions.
+// record of, each of its eight waves 16 of the output's dimensions at a time.  Lanes lie along query rows and then along
+// parts, each with a running maximum and sum of its own, so that all loads are independent of one another; a butterfly adds the
+// lanes of a row.  (Most workgroups find no record, so few and large ones: 64 parts of 5 rows, 8 such jobs took 12 us
+// with a workgroup per 16 dimensions.)
 template <int TR>
-__global__ void __launch_bounds__(256) k_paged_join(PagedArgs a) {
+__global__ void __launch_bounds__(512) k_paged_join(PagedArgs a) {
+  constexpr int RB = TR < 64 ? TR : 64;  // rows side by side in a wave
   const PagedRecord r = a.rec[blockIdx.x];
   if (r.last == 0) return;
-  const PagedSeq q = paged_seq(a, r.seq);
-  const int dh = a.c.head_dim, rows = min(TR, q.rows * a.rep - r.tile * TR), n = r.last - (int)blockIdx.x + 1;
-  int rb = 1, parts = 1;
-  while (rb < rows) rb *= 2;
-  while (parts < n && parts < 8 && 2 * parts * rb <= 64) parts *= 2;
-  const int row = threadIdx.x & (rb - 1), part = (threadIdx.x / rb) & (parts - 1), d0 = threadIdx.x / (rb * parts);
-  const int w0 = blockIdx.x;
-  const auto slot_of = [&](int i) { return i == 0 ? 2 * w0 + 1 : 2 * (w0 + i); };
-  float m = -INFINITY, l = 0.f;
-  for (int i = part; i < n; i += parts) m = fmaxf(m, a.part_ml[(slot_of(i) * 2) * TR + row]);
-  for (int o = rb; o < rb * parts; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-  const float m_ref = m == -INFINITY ? 0.f : m;
-  for (int i = part; i < n; i += parts)
-    l += a.part_ml[(slot_of(i) * 2 + 1) * TR + row] * __builtin_amdgcn_exp2f(a.part_ml[(slot_of(i) * 2) * TR + row] - m_ref);
-  for (int o = rb; o < rb * parts; o <<= 1) l += __shfl_xor(l, o, 64);
-  const int x = r.tile * TR + row, token = (int)div_by(min(x, q.rows * a.rep - 1), a.by_rep);
-  const int head = r.head * a.rep + x - token * a.rep;
-  const float inv = l != 0.f ? 1.f / l : 0.f;
-  const int quarter = dh / 16;  // groups of four dimensions per workgroup
-  for (int d4 = blockIdx.y * quarter + d0; d4 < (blockIdx.y + 1) * quarter; d4 += 256 / (rb * parts)) {
-    f32x4 o{0.f, 0.f, 0.f, 0.f};
+  const int quads = a.c.head_dim / 4, n = r.last - (int)blockIdx.x + 1, w0 = blockIdx.x;
+  const int lane = threadIdx.x & 63;
+  int rb = 1;
+  while (rb < min(r.n, RB)) rb *= 2;
+  const int part0 = lane / rb, step = 64 / rb;
+  for (int q0 = (threadIdx.x >> 6) * 4; q0 < quads; q0 += 32)
+    for (int base = 0; base < r.n; base += rb) {
+      const int row = base + (lane & (rb - 1));
+      const bool valid = row < r.n;
+      float m = -INFINITY, l = 0.f;
+      f32x4 o[4] = {};
+      if (valid) {
 #pragma unroll 4
-    for (int i = part; i < n; i += parts) {
-      const float w = __builtin_amdgcn_exp2f(a.part_ml[(slot_of(i) * 2) * TR + row] - m_ref);
-      const f32x4 v = *reinterpret_cast<const f32x4*>(a.part_o + (((int64_t)slot_of(i) * (dh / 4) + d4) * TR + row) * 4);
-      o += w == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : v * w;
-    }
-    for (int s = rb; s < rb * parts; s <<= 1)
+        for (int i = part0; i < n; i += step) {
+          const int64_t slot = i == 0 ? 2 * w0 + 1 : 2 * (w0 + i);
+          const float mi = a.part_ml[slot * 2 * TR + row], li = a.part_ml[(slot * 2 + 1) * TR + row];
+          f32x4 v[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], s, 64);
-    if (part != 0 || row >= rows) continue;
-    o *= inv;
-    const int64_t o_at = (int64_t)(q.row0 + token) * a.out_stride + (int64_t)head * dh + d4 * 4;
-    if (a.dtype == KEEP_F32)
-      *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + o_at) = o;
-    else
-      *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + o_at) =
-          make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]));
-    if (d4 == 0 && a.lse)
-      a.lse[(int64_t)(q.row0 + token) * a.n_q_heads + head] = 0.6931471805599453f * (m + log2f(l));
-  }
+          for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const f32x4*>(a.part_o + ((slot * quads + q0 + j) * TR + row) * 4);
+          const float m_new = fmaxf(m, mi), ref = m_new == -INFINITY ? 0.f : m_new;
+          const float old = __builtin_amdgcn_exp2f(m - ref), now = __builtin_amdgcn_exp2f(mi - ref);
+          l = l * old + li * now;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[j] = o[j] * old + (now == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : v[j] * now);
+          m = m_new;
+        }
+      }
+      const float m0 = m;
+      for (int s = rb; s < 64; s <<= 1) m = fmaxf(m, __shfl_xor(m, s, 64));
+      const float scale = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m0 - m);
+      l *= scale;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[j] *= scale;
+      for (int s = rb; s < 64; s <<= 1) {
+        l += __shfl_xor(l, s, 64);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[j][e] += __shfl_xor(o[j][e], s, 64);
+      }
+      if (!valid || lane >= rb) continue;
+      const int x = r.x0 + row, token = (int)div_by(x, a.by_rep), head = r.head * a.rep + x - token * a.rep;
+      const int64_t o_at = (int64_t)(r.row0 + token) * a.out_stride + (int64_t)head * a.c.head_dim + q0 * 4;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (l != 0.f) o[j] /= l;
+        if (a.dtype == KEEP_F32)
+          *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + o_at + 4 * j) = o[j];
+        else
+          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + o_at + 4 * j) =
+              make_uint2(pack_bf16x2(o[j][0], o[j][1]), pack_bf16x2(o[j][2], o[j][3]));
+      }
+      if (q0 == 0 && a.lse) a.lse[(int64_t)(r.row0 + token) * a.n_q_heads + head] = 0.6931471805599453f * (m + log2f(l));
+    }
 }
 
 uint64_t part_bytes(int tr, int dh) { return (uint64_t)2 * PAGED_WORKERS * tr * (dh + 2) * sizeof(float); }
@@ -246,7 +262,7 @@ void launch_paged_generic(const PagedArgs& a, hipStream_t s) {
 
 void launch_paged_join(const PagedArgs& a, int rows, hipStream_t s) {
   const auto kernel = rows == 16 ? k_paged_join<16> : k_paged_join<32>;
-  hipLaunchKernelGGL(kernel, dim3(PAGED_WORKERS, 4), dim3(256), 0, s, a);
+  hipLaunchKernelGGL(kernel, dim3(PAGED_WORKERS), dim3(512), 0, s, a);
 }
 
 }  // namespace keep
