@@ -2,10 +2,12 @@
 //
 // Work.  A job is (sequence, key/value head, tile of TR query rows); a query row is a token paired with one of the head's query
 // heads.  A job takes as many units as it has key tiles of KT keys between the first key its rows may see and the
-// last, at least one (so that rows which see nothing are written too).  All units of a launch, in the order sequence,
-// head, tile, key, are dealt to the workers (workgroups; no more than there are units) in equal runs: lengths differ by orders of magnitude from
+// last, at least one (so that rows which see nothing are written too).  The work of a launch, in the order sequence, head,
+// tile, key, is dealt to the workers (workgroups) in equal runs: lengths differ by orders of magnitude from
 // sequence to sequence, and their division has to come from device memory, where a captured graph finds the
 // step's own.  Every worker forms the division for itself: sums per sequence in LDS, a scan, then its own place.
+// Beginning a job takes about as long as a unit (tables, queries, the first loads, the output), so a job weighs one step more than
+// its units, the first of them without keys.
 //
 // A job cut by a border between runs leaves one partial result per worker: unnormalised output, running maximum and sum.  A
 // worker cuts at most the job it begins with (slot 2 w) and the one it ends with (slot 2 w + 1); the worker a cut job begins in
@@ -75,23 +77,24 @@ __device__ __forceinline__ int paged_tiles(const PagedArgs& a, const PagedSeq& q
   return (q.rows * a.rep + TR - 1) / TR;
 }
 
-// Every worker that takes part has a unit at least
+// Every worker that takes part has a step at least
 __device__ __forceinline__ uint64_t paged_workers(uint64_t total) { return min(total, (uint64_t)PAGED_WORKERS); }
-// The worker that takes unit v: the largest w with w * total / workers <= v
+// The worker that takes step v: the largest w with w * total / workers <= v
 __device__ __forceinline__ int paged_worker_of(uint64_t v, uint64_t total) {
   return (int)(((v + 1) * paged_workers(total) - 1) / total);
 }
 
 struct PagedPlace {    // where a worker begins, and how far it goes
-  uint64_t total;      // units of the launch
+  uint64_t total;      // steps of the launch
   uint64_t begin, end; // this worker's run
   int seq, head, tile;
-  int unit;            // units of the first job that earlier workers take
+  int step;            // steps of the first job that earlier workers take
 };
 
-// Called by all 256 threads; lds: 8 * (n_seqs + 260) bytes, free again after the caller's next barrier.
+// Called by all 256 threads; lds: 8 * (n_seqs + 260) bytes, free again after the caller's next barrier.  q: the sequence the
+// worker begins with.
 template <int TR, int KT>
-__device__ __forceinline__ PagedPlace paged_place(const PagedArgs& a, int worker, uint64_t* lds) {
+__device__ __forceinline__ PagedPlace paged_place(const PagedArgs& a, int worker, uint64_t* lds, PagedSeq& q) {
   const int tid = threadIdx.x;
   uint64_t* sums = lds + 260;
   for (int s = tid; s < a.n_seqs; s += 256) sums[s] = 0;
@@ -100,13 +103,13 @@ __device__ __forceinline__ PagedPlace paged_place(const PagedArgs& a, int worker
   int share = 1;
   while (share * 2 * a.n_seqs <= 256) share *= 2;
   for (int s = tid / share; s < a.n_seqs; s += 256 / share) {
-    const PagedSeq q = paged_seq(a, s);
-    const int tiles = paged_tiles<TR>(a, q);
+    const PagedSeq one = paged_seq(a, s);
+    const int tiles = paged_tiles<TR>(a, one);
     uint64_t sum = 0;
-    for (int t = tid % share; t < tiles; t += share) {
+    for (int t = tid & (share - 1); t < tiles; t += share) {
       int first, units;
-      paged_span<TR, KT>(a, q, t, first, units);
-      sum += units;
+      paged_span<TR, KT>(a, one, t, first, units);
+      sum += units + 1;
     }
     if (sum) atomicAdd(reinterpret_cast<unsigned long long*>(sums + s), (unsigned long long)sum);
   }
@@ -127,62 +130,72 @@ __device__ __forceinline__ PagedPlace paged_place(const PagedArgs& a, int worker
     if (w < (tid >> 6)) before += lds[w];
     total += lds[w];
   }
-  before -= own;
-  PagedPlace p;
-  p.total = total * a.c.n_kv_heads;
-  const uint64_t workers = paged_workers(p.total);
-  p.begin = p.end = p.total;
-  if ((uint64_t)worker < workers) {
-    p.begin = p.total * worker / workers;
-    p.end = p.total * (worker + 1) / workers;
-  }
-  if (tid == 0) lds[8] = 0, lds[9] = 0;
-  __syncthreads();
-  before *= a.c.n_kv_heads;
+  before = (before - own) * a.c.n_kv_heads;
   own *= a.c.n_kv_heads;
-  if (own && p.begin >= before && p.begin < before + own) {
-    int s = s0;
+  PagedPlace p{};
+  p.total = paged_uniform(total * a.c.n_kv_heads);
+  static_assert((PAGED_WORKERS & (PAGED_WORKERS - 1)) == 0, "the runs are found by shifts");
+  const bool many = p.total >= PAGED_WORKERS;
+  p.begin = many ? p.total * worker / PAGED_WORKERS : min((uint64_t)worker, p.total);
+  p.end = many ? p.total * (worker + 1) / PAGED_WORKERS : min((uint64_t)worker + 1, p.total);
+  if (p.begin >= p.end) return p;
+  if (p.begin >= before && p.begin < before + own) {  // one thread
+    int s = s0, head = 0;
     uint64_t at = p.begin - before;
     while (at >= sums[s] * a.c.n_kv_heads) at -= sums[s++] * a.c.n_kv_heads;
-    lds[8] = s;
+    while (at >= sums[s]) at -= sums[s], ++head;
+    lds[8] = (uint64_t)(uint32_t)head << 32 | (uint32_t)s;
     lds[9] = at;
-    lds[10] = sums[s];
   }
   __syncthreads();
-  p.seq = p.head = p.tile = p.unit = 0;
-  if (p.begin < p.end) {
-    p.seq = (int)lds[8];
-    p.head = (int)(lds[9] / lds[10]);
-    uint64_t at = lds[9] - p.head * lds[10];
-    // the tile: 64 at a time, a lane each
-    const PagedSeq q = paged_seq(a, p.seq);
-    const int tiles = paged_tiles<TR>(a, q), lane = tid & 63;
-    for (int t0 = 0;; t0 += 64) {
-      int first, units = 0;
-      if (t0 + lane < tiles) paged_span<TR, KT>(a, q, t0 + lane, first, units);
-      uint64_t sum = units;
-      for (int o = 1; o < 64; o <<= 1) {
-        const uint64_t up = __shfl_up((unsigned long long)sum, o, 64);
-        if (lane >= o) sum += up;
-      }
-      const uint64_t past = __ballot(sum > at);
-      if (past || t0 + 64 >= tiles) {
-        const int l = past ? __ffsll((unsigned long long)past) - 1 : 0;
-        p.tile = t0 + l;
-        p.unit = (int)(at - (l ? __shfl((unsigned long long)sum, l - 1, 64) : 0));
-        break;
-      }
-      at -= __shfl((unsigned long long)sum, 63, 64);
+  p.seq = paged_uniform((int)lds[8]);
+  p.head = paged_uniform((int)(lds[8] >> 32));
+  uint64_t at = paged_uniform(lds[9]);
+  // the tile: 64 at a time, a lane each
+  q = paged_uniform(paged_seq(a, p.seq));
+  const int tiles = paged_tiles<TR>(a, q), lane = tid & 63;
+  for (int t0 = 0; t0 < tiles; t0 += 64) {
+    int first, units = -1;
+    if (t0 + lane < tiles) paged_span<TR, KT>(a, q, t0 + lane, first, units);
+    uint64_t sum = units + 1;
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint64_t up = __shfl_up((unsigned long long)sum, o, 64);
+      if (lane >= o) sum += up;
     }
+    const uint64_t past = __ballot(sum > at);
+    if (past) {
+      const int l = __ffsll((unsigned long long)past) - 1;
+      p.tile = t0 + l;
+      p.step = paged_uniform((int)(at - (l ? __shfl((unsigned long long)sum, l - 1, 64) : 0)));
+      break;
+    }
+    at -= paged_uniform((uint64_t)__shfl((unsigned long long)sum, 63, 64));
   }
-  return PagedPlace{paged_uniform(p.total), paged_uniform(p.begin), paged_uniform(p.end),  paged_uniform(p.seq),
-                    paged_uniform(p.head),  paged_uniform(p.tile),  paged_uniform(p.unit)};
+  return p;
+}
+
+// The part of a job that a worker takes: units [u0, u1), none where it has the first step alone
+struct PagedPart {
+  int first, units, u0, u1;  // units: of the whole job; first: key tile of unit 0
+  int steps;                 // steps of the worker's run that it uses up
+  uint64_t last;             // the job's last step
+};
+template <int TR, int KT>
+__device__ __forceinline__ PagedPart paged_part(const PagedArgs& a, const PagedPlace& p, const PagedSeq& q, uint64_t at) {
+  PagedPart r;
+  paged_span<TR, KT>(a, q, p.tile, r.first, r.units);
+  const int c1 = (int)min((uint64_t)r.units + 1, p.step + (p.end - at));
+  r.u0 = max(p.step - 1, 0);
+  r.u1 = c1 - 1;
+  r.steps = c1 - p.step;
+  r.last = at - p.step + r.units;
+  return r;
 }
 
 // The job behind (seq, head, tile); sequences without rows are passed over.  Only called where another job exists.
 template <int TR>
 __device__ __forceinline__ void paged_next(const PagedArgs& a, PagedPlace& p, PagedSeq& q) {
-  p.unit = 0;
+  p.step = 0;
   if (++p.tile < paged_tiles<TR>(a, q)) return;
   p.tile = 0;
   if (++p.head < a.c.n_kv_heads) return;
@@ -204,13 +217,13 @@ typedef __attribute__((ext_vector_type(4))) float paged_f32x4;
 // The four waves' parts of a job (each of other keys), added in their order: the job's result, or a partial one where the job
 // was cut.  so: LDS [4 waves][head_dim / 4][TR][4]; sml: LDS [2][4 waves][TR], maxima and sums.
 template <int TR>
-__device__ __forceinline__ void paged_finish(const PagedArgs& a, const PagedPlace& p, const PagedSeq& q, int worker, uint64_t at,
-                                             int u0, int u1, int units, const float* so, const float* sml) {
+__device__ __forceinline__ void paged_finish(const PagedArgs& a, const PagedPlace& p, const PagedSeq& q, const PagedPart& part,
+                                             int worker, const float* so, const float* sml) {
   const int tid = threadIdx.x, row = tid % TR, quads = a.c.head_dim / 4;
   const int x = p.tile * TR + row;
-  const bool valid = x < q.rows * a.rep, whole = u0 == 0 && u1 == units;
+  const bool valid = x < q.rows * a.rep, whole = part.u0 == 0 && part.u1 == part.units;
   const int token = valid ? (int)div_by(x, a.by_rep) : 0, head = p.head * a.rep + (valid ? x - token * a.rep : 0);
-  const int64_t slot = 2 * worker + (u0 == 0 ? 1 : 0);
+  const int64_t slot = 2 * worker + (part.u0 == 0 ? 1 : 0);
   float mw[4], m = -INFINITY, l = 0.f;
 #pragma unroll
   for (int w = 0; w < 4; ++w) m = fmaxf(m, mw[w] = sml[w * TR + row]);
@@ -247,8 +260,8 @@ __device__ __forceinline__ void paged_finish(const PagedArgs& a, const PagedPlac
       a.lse[(int64_t)(q.row0 + token) * a.n_q_heads + head] = 0.6931471805599453f * (m + log2f(l));
     }
   }
-  if (tid == 0 && u0 == 0 && !whole)
-    a.rec[worker] = PagedRecord{paged_worker_of(at + units - 1, p.total), q.row0, p.tile * TR, min(TR, q.rows * a.rep - p.tile * TR),
+  if (tid == 0 && part.u0 == 0 && !whole)
+    a.rec[worker] = PagedRecord{paged_worker_of(part.last, p.total), q.row0, p.tile * TR, min(TR, q.rows * a.rep - p.tile * TR),
                                 p.head};
 }
 

@@ -54,17 +54,16 @@ __global__ void __launch_bounds__(256) k_paged_generic(PagedArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, g = lane >> 4;
   const int dh = a.c.head_dim, nd = dh / 16, stride = dh + 4;
   const int worker = blockIdx.x;
-  PagedPlace p = paged_place<GT_ROWS, GT_KEYS>(a, worker, reinterpret_cast<uint64_t*>(lds));
+  PagedSeq q;
+  PagedPlace p = paged_place<GT_ROWS, GT_KEYS>(a, worker, reinterpret_cast<uint64_t*>(lds), q);
   if (tid == 0) a.rec[worker].last = 0;
   if (p.begin >= p.end) return;
   float* sk = lds;
   float* sv = lds + GT_KEYS * stride;
   float* sml = sv + GT_KEYS * stride;  // [2][4 waves][16]
-  PagedSeq q = paged_uniform(paged_seq(a, p.seq));
   for (uint64_t at = p.begin;;) {
-    int first, units;
-    paged_span<GT_ROWS, GT_KEYS>(a, q, p.tile, first, units);
-    const int u0 = p.unit, u1 = (int)min((uint64_t)units, u0 + (p.end - at));
+    const PagedPart part = paged_part<GT_ROWS, GT_KEYS>(a, p, q, at);
+    if (part.u0 == part.u1) break;  // (the run's last step)
     const int x = p.tile * GT_ROWS + col;
     const bool valid = x < q.rows * a.rep;
     const int token = valid ? (int)div_by(x, a.by_rep) : 0;
@@ -81,7 +80,7 @@ __global__ void __launch_bounds__(256) k_paged_generic(PagedArgs a) {
     float m = -INFINITY, l = 0.f;
     const int32_t* table = a.table + (int64_t)p.seq * a.max_pages;
 
-    for (int kt = first + u0; kt < first + u1; ++kt) {
+    for (int kt = part.first + part.u0; kt < part.first + part.u1; ++kt) {
       __syncthreads();  // the tile before has been read
       if (tid == 0) odd = 0;
       __syncthreads();
@@ -171,8 +170,8 @@ __global__ void __launch_bounds__(256) k_paged_generic(PagedArgs a) {
     for (int i = 0; i < ND; ++i)
       if (i < nd) *reinterpret_cast<f32x4*>(so + ((wave * (dh / 4) + 4 * i + g) * 16 + col) * 4) = acc[i];
     __syncthreads();
-    paged_finish<GT_ROWS>(a, p, q, worker, at, u0, u1, units, so, sml);
-    at += u1 - u0;
+    paged_finish<GT_ROWS>(a, p, q, part, worker, so, sml);
+    at += part.steps;
     if (at >= p.end) break;
     paged_next<GT_ROWS>(a, p, q);
   }

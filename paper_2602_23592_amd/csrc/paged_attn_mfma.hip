@@ -114,7 +114,8 @@ __global__ void __launch_bounds__(256, 2) k_paged_few(PagedArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, g = lane >> 4;
   // The workgroups of an XCD (blockIdx % 8) take neighbouring runs: one head's tiles read the same keys from its L2
   const int worker = (blockIdx.x & 7) * (PAGED_WORKERS / 8) + (blockIdx.x >> 3);
-  PagedPlace p = paged_place<TR, UNIT>(a, worker, reinterpret_cast<uint64_t*>(lds));
+  PagedSeq q;
+  PagedPlace p = paged_place<TR, UNIT>(a, worker, reinterpret_cast<uint64_t*>(lds), q);
   if (tid == 0) a.rec[worker].last = 0;
   if (p.begin >= p.end) return;
   char* ring = lds + wave * F::WAVE;  // [NS] K slices, [NS] V slices, [NS] scales (32 of keys, 32 of values)
@@ -124,12 +125,11 @@ __global__ void __launch_bounds__(256, 2) k_paged_few(PagedArgs a) {
   const char* k_base = static_cast<const char*>(a.c.k);
   const char* v_base = static_cast<const char*>(a.c.v);
   const int block_units = (int)max((int64_t)1, min((int64_t)1 << 20, (int64_t)(TABLE - 2) * a.c.page_size / UNIT));
-  PagedSeq q = paged_uniform(paged_seq(a, p.seq));
 
   for (uint64_t at = p.begin;;) {
-    int first, units;
-    paged_span<TR, UNIT>(a, q, p.tile, first, units);
-    const int u0 = p.unit, u1 = (int)min((uint64_t)units, u0 + (p.end - at));
+    const PagedPart part = paged_part<TR, UNIT>(a, p, q, at);
+    if (part.u0 == part.u1) break;  // (the run's last step)
+    const int first = part.first, u1 = part.u1;
     // ---- this lane's query rows
     int pos[RB], lo[RB];
     bf16x8 qf[RB][KS];
@@ -146,12 +146,6 @@ __global__ void __launch_bounds__(256, 2) k_paged_few(PagedArgs a) {
       for (int ks = 0; ks < KS; ++ks)  // the dimensions that the K operand of step ks holds
         qf[b][ks] = *reinterpret_cast<const bf16x8*>(qp + (F::WIDE ? ks * 32 + g * 8 : (ks >> 1) * 64 + g * 16 + (ks & 1) * 8));
     }
-    // (the queries are in registers before the slices' loads begin: the compiler would wait for them, and so for those, in
-    // every slice)
-#pragma unroll
-    for (int b = 0; b < RB; ++b)
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[b][ks]));
     int max_pos, min_pos, max_lo;  // over the tile
     {
       const int x1 = min(q.rows * a.rep, (p.tile + 1) * TR) - 1;
@@ -170,13 +164,19 @@ __global__ void __launch_bounds__(256, 2) k_paged_few(PagedArgs a) {
     const int32_t* table = a.table + (int64_t)p.seq * a.max_pages;
     const int64_t head_at = (int64_t)p.head * a.c.head_stride * (F::WIDE ? 2 : 1);
 
-    for (int ub = u0; ub < u1; ub += block_units) {
+    for (int ub = part.u0; ub < u1; ub += block_units) {
       const int ue = min(u1, ub + block_units);
       const int page0 = (int)div_by((uint32_t)(first + ub) * UNIT, a.by_page);
       const int page1 = (int)div_by((uint32_t)min((int64_t)(first + ue) * UNIT - 1, (int64_t)max(q.len, 1) - 1), a.by_page);
       __syncthreads();  // earlier entries, or the outputs of the job before, have been read
       for (int i = tid; i <= page1 - page0; i += 256) tbl[i] = min(max(table[page0 + i], 0), a.c.n_pages - 1);
       __syncthreads();
+      // (the queries, requested before the table, are in registers before the slices' loads begin: the compiler would wait for
+      // them, and so for those, in every slice)
+#pragma unroll
+      for (int b = 0; b < RB; ++b)
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[b][ks]));
       // ---- this wave's slices: keys key0 + UNIT * t, while some row sees them
       const int key0 = (first + ub) * UNIT + wave * SLICE;
       const int n = key0 > max_pos ? 0 : min(ue - ub, (max_pos - key0) / UNIT + 1);
@@ -401,8 +401,8 @@ __global__ void __launch_bounds__(256, 2) k_paged_few(PagedArgs a) {
         *reinterpret_cast<f32x4*>(so + ((wave * (DH / 4) + 4 * i + g) * TR + b * 16 + col) * 4) = acc[b][i];
     }
     __syncthreads();
-    paged_finish<TR>(a, p, q, worker, at, u0, u1, units, so, sml);
-    at += u1 - u0;
+    paged_finish<TR>(a, p, q, part, worker, so, sml);
+    at += part.steps;
     if (at >= p.end) break;
     paged_next<TR>(a, p, q);
   }
