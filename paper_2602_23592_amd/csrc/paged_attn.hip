@@ -244,6 +244,13 @@ __global__ void __launch_bounds__(512) k_paged_join(PagedArgs a) {
 }
 
 uint64_t part_bytes(int tr, int dh) { return (uint64_t)2 * PAGED_WORKERS * tr * (dh + 2) * sizeof(float); }
+// caches that paged_attn_mfma.hip has a kernel for (with bf16 queries); offsets in 16 bytes fit 32 bits
+bool has_mfma(const keep_paged_cache* c) {
+  const int64_t span = (int64_t)(c->n_pages - 1) * c->page_stride + (int64_t)(c->n_kv_heads - 1) * c->head_stride +
+                       (int64_t)(c->page_size - 1) * c->token_stride + c->head_dim;
+  return c->format != KEEP_CACHE_F32 && (c->head_dim == 64 || c->head_dim == 128) &&
+         span * format_size(c->format) < (int64_t)64 << 30;
+}
 constexpr uint64_t REC_BYTES = (PAGED_WORKERS * sizeof(PagedRecord) + 255) & ~(uint64_t)255;
 
 }  // namespace
@@ -260,7 +267,7 @@ void launch_paged_generic(const PagedArgs& a, hipStream_t s) {
 }
 
 void launch_paged_join(const PagedArgs& a, int rows, hipStream_t s) {
-  const auto kernel = rows == 16 ? k_paged_join<16> : k_paged_join<32>;
+  const auto kernel = rows == 16 ? k_paged_join<16> : rows == 32 ? k_paged_join<32> : k_paged_join<128>;
   hipLaunchKernelGGL(kernel, dim3(PAGED_WORKERS), dim3(512), 0, s, a);
 }
 
@@ -271,7 +278,7 @@ using namespace keep;
 extern "C" uint64_t keep_paged_attention_workspace_bytes(const keep_paged_cache* cache, int32_t n_q_heads, int32_t n_seqs) {
   if (check_cache(cache, "keep_paged_attention_workspace_bytes") != KEEP_OK) return 0;
   if (n_q_heads < 1 || n_q_heads % cache->n_kv_heads || n_seqs < 0 || n_seqs > KEEP_PAGED_MAX_SEQS) return 0;
-  return REC_BYTES + part_bytes(32, cache->head_dim);
+  return REC_BYTES + part_bytes(has_mfma(cache) ? 128 : GT_ROWS, cache->head_dim);
 }
 
 extern "C" keep_status keep_paged_attention(const keep_paged_attention_desc* d, const keep_paged_cache* cache, const void* q,
@@ -333,16 +340,14 @@ extern "C" keep_status keep_paged_attention(const keep_paged_attention_desc* d, 
   a.rec = reinterpret_cast<PagedRecord*>(ws);
   a.part_ml = reinterpret_cast<float*>(ws + REC_BYTES);
   if (!format_scaled(cache->format)) a.c.k_scale = a.c.v_scale = nullptr;
-  // The bf16 matrix instruction where it has a kernel.  Tiles of 16 query rows while sequences bring no more on average
-  // (one to a few tokens), else of 32.
-  const int64_t span = (int64_t)(cache->n_pages - 1) * cache->page_stride + (int64_t)(cache->n_kv_heads - 1) * cache->head_stride +
-                       (int64_t)(cache->page_size - 1) * cache->token_stride + cache->head_dim;
-  const bool mfma = d->dtype == KEEP_BF16 && cache->format != KEEP_CACHE_F32 &&
-                    (cache->head_dim == 64 || cache->head_dim == 128) && span * format_size(cache->format) < (int64_t)64 << 30;
-  const int rows = !mfma || d->n_rows * (int64_t)a.rep <= 16 * (int64_t)d->n_seqs ? 16 : 32;
+  // The bf16 matrix instruction where it has a kernel.  Tiles of 16 query rows while sequences bring no more on average (one to a
+  // few tokens), then of 32, then of 128.
+  const bool mfma = d->dtype == KEEP_BF16 && has_mfma(cache);
+  const int64_t mean = (d->n_rows * (int64_t)a.rep + d->n_seqs - 1) / d->n_seqs;
+  const int rows = !mfma || mean <= 16 ? 16 : mean <= 32 ? 32 : 128;
   a.part_o = a.part_ml + (size_t)2 * PAGED_WORKERS * 2 * rows;
   if (mfma)
-    launch_paged_few(a, rows, static_cast<hipStream_t>(stream));
+    launch_paged_mfma(a, rows, static_cast<hipStream_t>(stream));
   else
     launch_paged_generic(a, static_cast<hipStream_t>(stream));
   return launched(me);

@@ -11,6 +11,11 @@
 // reads (ds_read_b64_tr_b16, _tr_b8).  8-bit codes become bf16 exactly (at most 8 significant bits) when they are read as
 // operands; a key's scale multiplies its scores, a value's scale its probability, in binary32.  Probabilities (with the
 // value's scale) are rounded to bf16 for the product, the row sums are taken before that.
+//
+// k_paged_many: tiles of 128 query rows, 32 per wave, over key tiles of 64 that the workgroup shares in LDS (two of them: the
+// next arrives while one is used), where the matrix instruction and the exponentials are the bound.  32x32x16: a lane owns a
+// query row (lane % 32) and half of the tile's keys, and again S^T = K . Q^T leaves the operand of O^T = V^T . P^T.
+// 8-bit codes become bf16 on their way into LDS, once for the four waves.
 #include "paged_attn.h"
 
 namespace keep {
@@ -21,6 +26,7 @@ typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((ext_vector_type(2))) int i32x2;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
 using f32x4 = paged_f32x4;
 typedef s16x4 __attribute__((address_space(3))) * lds_s16x4;
 typedef i32x2 __attribute__((address_space(3))) * lds_i32x2;
@@ -408,6 +414,339 @@ __global__ void __launch_bounds__(256, 2) k_paged_few(PagedArgs a) {
   }
 }
 
+constexpr int MT_ROWS = 128, MT_KEYS = 64;
+
+template <int DH, int FMT>
+struct Many {
+  static constexpr bool WIDE = FMT == KEEP_CACHE_BF16;
+  static constexpr int ROW = DH * 2, CH = ROW / 16;             // bytes and chunks of a key in LDS (bf16)
+  static constexpr int TILE = MT_KEYS * ROW;                    // bytes of a tile of K or of V
+  static constexpr int SC = 4 * TILE, TBL = SC + 2 * 2 * MT_KEYS * 4, LDS = TBL + TABLE * 4;
+};
+
+// Where a tile's 16-byte chunks lie: a K read is 32 rows at one chunk (16 at a time), a transposing V read four rows of four chunks.
+template <int CH>
+__device__ __forceinline__ int mk_chunk(int row, int c) {
+  return CH == 16 ? c ^ (row & 15) : c ^ ((row >> 1) & 7);
+}
+template <int CH>
+__device__ __forceinline__ int mv_chunk(int row, int c) {
+  return CH == 16 ? c ^ (4 * (row & 3)) : c ^ (4 * ((row >> 1) & 1));
+}
+
+template <int DH, int FMT>
+__global__ void __launch_bounds__(256, 2) k_paged_many(PagedArgs a) {
+  using F = Many<DH, FMT>;
+  constexpr int TR = MT_ROWS, KT = MT_KEYS, ROW = F::ROW, CH = F::CH, KS = DH / 16, NT = DH / 32;
+  extern __shared__ __attribute__((aligned(256))) char lds[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, lq = lane & 31;
+  const int worker = (blockIdx.x & 7) * (PAGED_WORKERS / 8) + (blockIdx.x >> 3);  // (neighbouring runs on one XCD)
+  PagedSeq q;
+  PagedPlace p = paged_place<TR, KT>(a, worker, reinterpret_cast<uint64_t*>(lds), q);
+  if (tid == 0) a.rec[worker].last = 0;
+  if (p.begin >= p.end) return;
+  float* scales = reinterpret_cast<float*>(lds + F::SC);  // [2 buffers][64 of keys (with the scores' factor), 64 of values]
+  int32_t* tbl = reinterpret_cast<int32_t*>(lds + F::TBL);
+  const uint32_t lds_at = __builtin_amdgcn_readfirstlane(lds_address(lds));
+  const int block_units = (int)max((int64_t)1, min((int64_t)1 << 20, (int64_t)(TABLE - 2) * a.c.page_size / KT));
+  const float factor = fabsf(a.scale_log2e);
+
+  // This lane's first operand chunks inside a tile: the others differ by one exclusive or, as the chunks' places do.  (Formed
+  // anew in every tile: kept, they would push registers out to memory.)
+  const int k_first = lq * ROW + mk_chunk<CH>(lq, g) * 16;
+  int v_first;
+  {
+    const int vr = 4 * g + ((lane & 15) >> 2), c = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    v_first = vr * ROW + mv_chunk<CH>(vr, c) * 16 + 8 * (lane & 1);
+  }
+
+  for (uint64_t at = p.begin;;) {
+    const PagedPart part = paged_part<TR, KT>(a, p, q, at);
+    if (part.u0 == part.u1) break;  // (the run's last step)
+    // ---- this lane's query row, and what the wave's rows see: keys up to pos, from lo on
+    const int rows = q.rows * a.rep;
+    int pos, lo;
+    int max_pos = -1, min_pos = -1, max_lo = 0, min_lo = 0;
+    {
+      const int x0 = p.tile * TR + wave * 32, x1 = min(rows, x0 + 32) - 1;
+      if (x0 < rows) {
+        min_pos = x1 - x0 < 31 ? -1 : q.len - q.rows + (int)div_by(x0, a.by_rep);  // (lanes without a row see nothing)
+        max_pos = q.len - q.rows + (int)div_by(x1, a.by_rep);
+        max_lo = a.window ? max(0, max_pos - a.window + 1) : 0;
+        min_lo = a.window ? max(0, q.len - q.rows + (int)div_by(x0, a.by_rep) - a.window + 1) : 0;
+      }
+    }
+    bf16x8 qf[KS];
+    {
+      const int x = p.tile * TR + wave * 32 + lq;
+      const bool valid = x < rows;
+      const int token = valid ? (int)div_by(x, a.by_rep) : 0, head = p.head * a.rep + (valid ? x - token * a.rep : 0);
+      pos = valid ? q.len - q.rows + token : -1;
+      lo = a.window ? max(0, pos - a.window + 1) : 0;
+      const __bf16* qp = static_cast<const __bf16*>(a.q) + (int64_t)(q.row0 + token) * a.q_stride + (int64_t)head * DH + g * 8;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        u32x4 u = *reinterpret_cast<const u32x4*>(qp + ks * 16);
+        if (F::WIDE && a.scale_log2e < 0.f) u ^= 0x80008000u;  // (the maximum is taken of products: their factor is positive)
+        qf[ks] = __builtin_bit_cast(bf16x8, u);
+      }
+    }
+    f32x16 acc[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[nt][e] = 0.f;
+    float m = -INFINITY, l = 0.f;
+    const int32_t* table = a.table + (int64_t)p.seq * a.max_pages;
+    const int64_t head_at = (int64_t)p.head * a.c.head_stride;
+
+    for (int ub = part.u0; ub < part.u1; ub += block_units) {
+      const int ue = min(part.u1, ub + block_units), kt0 = part.first + ub, kt1 = part.first + ue;
+      const int page0 = (int)div_by((uint32_t)kt0 * KT, a.by_page);
+      const int page1 = (int)div_by((uint32_t)min((int64_t)kt1 * KT - 1, (int64_t)max(q.len, 1) - 1), a.by_page);
+      __syncthreads();  // earlier entries, or the tiles of the job before, have been read
+      for (int i = tid; i <= page1 - page0; i += 256) tbl[i] = min(max(table[page0 + i], 0), a.c.n_pages - 1);
+      __syncthreads();
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[ks]));  // (in registers before the tiles' loads begin)
+
+      // ---- tile kt to buffer `buf`.  bf16: straight to LDS, a wave 16 rows of it.  8 bits: 16 codes of a row per load, kept in
+      // registers until the other buffer has been used.  Keys past the end read the last one again and are masked.
+      constexpr int LPR = DH / 16, RPL = 256 / LPR, NL = KT / RPL;  // 8 bits: threads per row, rows of a load, loads
+      u32x4 kc[F::WIDE ? 1 : NL], vc[F::WIDE ? 1 : NL];
+      float sc = 0.f;
+      const auto place = [&](int key, int64_t& scale) {
+        const int n = (int)div_by(key, a.by_page), in = key - n * a.c.page_size, page = tbl[n - page0];
+        scale = ((int64_t)page * a.c.n_kv_heads + p.head) * a.c.page_size + in;
+        return page * a.c.page_stride + in * a.c.token_stride + head_at;
+      };
+      const auto request = [&](int kt, int buf) {
+        const int last = max(q.len, 1) - 1;
+        int64_t s;
+        if constexpr (F::WIDE) {
+          constexpr int PER = 64 / CH, NI = 16 / PER;  // rows of a load, loads of a wave's 16 rows
+#pragma unroll
+          for (int i = 0; i < NI; ++i) {
+            const int row = wave * 16 + i * PER + lane / CH;
+            const int64_t e = place(min(kt * KT + row, last), s);
+            const uint32_t to = lds_at + buf * 2 * F::TILE + (wave * 16 + i * PER) * ROW;
+            load_lds16(static_cast<const __bf16*>(a.c.k) + e + mk_chunk<CH>(row, lane % CH) * 8, to);
+            load_lds16(static_cast<const __bf16*>(a.c.v) + e + mv_chunk<CH>(row, lane % CH) * 8, to + F::TILE);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < NL; ++i) {
+            const int64_t e = place(min(kt * KT + i * RPL + tid / LPR, last), s) + (tid % LPR) * 16;
+            kc[i] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(a.c.k) + e);
+            vc[i] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(a.c.v) + e);
+          }
+          if (tid < 2 * KT) {
+            place(min(kt * KT + (tid & (KT - 1)), last), s);
+            sc = tid < KT ? a.c.k_scale[s] * a.scale_log2e : a.c.v_scale[s];
+          }
+        }
+      };
+      const auto arrive = [&](int buf) {
+        if constexpr (F::WIDE) {
+          vm_wait<0>();
+        } else {
+          char* to = lds + buf * 2 * F::TILE;
+#pragma unroll
+          for (int i = 0; i < NL; ++i) {
+            const int row = i * RPL + tid / LPR, c = 2 * (tid % LPR);
+            *reinterpret_cast<bf16x8*>(to + row * ROW + mk_chunk<CH>(row, c) * 16) = codes8<FMT>(kc[i][0], kc[i][1]);
+            *reinterpret_cast<bf16x8*>(to + row * ROW + mk_chunk<CH>(row, c + 1) * 16) = codes8<FMT>(kc[i][2], kc[i][3]);
+            *reinterpret_cast<bf16x8*>(to + F::TILE + row * ROW + mv_chunk<CH>(row, c) * 16) = codes8<FMT>(vc[i][0], vc[i][1]);
+            *reinterpret_cast<bf16x8*>(to + F::TILE + row * ROW + mv_chunk<CH>(row, c + 1) * 16) = codes8<FMT>(vc[i][2], vc[i][3]);
+          }
+          if (tid < 2 * KT) scales[buf * 2 * KT + tid] = sc;
+        }
+      };
+
+      request(kt0, 0);
+      arrive(0);
+      __syncthreads();
+      for (int kt = kt0; kt < kt1; ++kt) {
+        const int cur = (kt - kt0) & 1, k0 = kt * KT;
+        // every wave finished reading the other buffer before the barrier that ended the last iteration
+        if (kt + 1 < kt1) request(kt + 1, cur ^ 1);
+        if (k0 <= max_pos && k0 + KT > min_lo) {
+          const char* sk = lds + cur * 2 * F::TILE;
+          const char* sv = sk + F::TILE;
+          const float* ksc = scales + cur * 2 * KT;
+          int k_at = k_first, v_at = v_first;
+          asm volatile("" : "+v"(k_at), "+v"(v_at));
+          f32x16 s[2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[h][e] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+              s[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(sk + h * 32 * ROW + (k_at ^ (ks * 32))), qf[ks],
+                                                             s[h], 0, 0, 0);
+          }
+          // ---- scores (8 bits: in the log2 domain already), mask, running maximum
+          if constexpr (!F::WIDE) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const f32x4 f = *reinterpret_cast<const f32x4*>(ksc + h * 32 + 8 * i + 4 * g);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[h][4 * i + e] *= f[e];
+              }
+          }
+          const bool masked = k0 + KT - 1 > min_pos || k0 < max_lo;
+          if (masked) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                const int key = k0 + h * 32 + 8 * (e >> 2) + 4 * g + (e & 3);
+                s[h][e] = key <= pos && key >= lo ? s[h][e] : -INFINITY;
+              }
+          }
+          float top = -INFINITY;
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) top = fmaxf(top, s[h][e]);
+          {
+            auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+            top = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+          }
+          if (F::WIDE) top *= factor;
+          const float m_new = fmaxf(m, top), ref = m_new == -INFINITY ? 0.f : m_new;
+          if (__ballot(m_new != m)) {  // rescale only where some row's maximum moved
+            const float alpha = __builtin_amdgcn_exp2f(m - ref);
+            l *= alpha;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int e = 0; e < 16; ++e) acc[nt][e] *= alpha;
+            m = m_new;
+          }
+          uint32_t pk[2][8];
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) {
+              float p0 = __builtin_amdgcn_exp2f(F::WIDE ? __builtin_fmaf(s[h][e], factor, -ref) : s[h][e] - ref);
+              float p1 = __builtin_amdgcn_exp2f(F::WIDE ? __builtin_fmaf(s[h][e + 1], factor, -ref) : s[h][e + 1] - ref);
+              l += p0 + p1;
+              if constexpr (!F::WIDE) {
+                const float* v = ksc + KT + h * 32 + 8 * (e >> 2) + 4 * g + (e & 3);
+                p0 = masked && s[h][e] == -INFINITY ? 0.f : p0 * v[0];  // (a scale of NaN stays with the rows that see the key)
+                p1 = masked && s[h][e + 1] == -INFINITY ? 0.f : p1 * v[1];
+              }
+              pk[h][e >> 1] = pack_bf16x2(p0, p1);
+            }
+          bool odd = false;
+          if (masked && FMT != KEEP_CACHE_INT8) {
+            // A product with a probability of zero would carry infinities and NaN to rows that do not see the key.
+            for (int i = lane; i < F::TILE / 16; i += 64) {
+              const u32x4 w = *reinterpret_cast<const u32x4*>(sv + i * 16);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) odd = odd || (w[e] & 0x7f80u) == 0x7f80u || (w[e] & 0x7f800000u) == 0x7f800000u;
+            }
+            odd = __ballot(odd) != 0;
+          }
+          if (!odd) {
+            // slot (g, i) of step s holds key 16 s + 8 (i / 4) + 4 g + i % 4: the keys of P^T's registers as they are
+#pragma unroll
+            for (int step = 0; step < 4; ++step) {
+              u32x4 pu;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) pu[i] = pk[step >> 1][(step & 1) * 4 + i];
+              const bf16x8 pf = __builtin_bit_cast(bf16x8, pu);
+              const char* vb = sv + step * 16 * ROW;
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) {
+                const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(vb + (v_at ^ (nt * 64))));
+                const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(vb + 8 * ROW + (v_at ^ (nt * 64))));
+                acc[nt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                    __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7)), pf, acc[nt], 0, 0, 0);
+              }
+            }
+          } else {
+#pragma unroll 1
+            for (int j = 0; j < KT; ++j) {  // a key at a time, for the rows that see it
+              uint32_t two = 0;  // key j lies in lane half (j / 4) % 2, element 4 (j % 32 / 8) + j % 4 of half-tile j / 32
+              const int want = (j >> 5) * 8 + ((j & 31) >> 3) * 2 + ((j & 3) >> 1);
+#pragma unroll
+              for (int i = 0; i < 16; ++i) two = want == i ? pk[i >> 3][i & 7] : two;
+              two = (uint32_t)__shfl((int)two, ((j >> 2) & 1) * 32 + lq, 64);
+              const float pj = bf16_bits_to_f32((uint16_t)(j & 1 ? two >> 16 : two));
+              const bool sees = k0 + j <= pos && k0 + j >= lo;
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {  // dimensions 32 nt + 8 i + 4 g + r
+                  const uint2 w = *reinterpret_cast<const uint2*>(sv + j * ROW + mv_chunk<CH>(j, 4 * nt + i) * 16 + 8 * g);
+                  const uint32_t u[2] = {w.x, w.y};
+#pragma unroll
+                  for (int r = 0; r < 4; ++r)
+                    acc[nt][4 * i + r] += sees ? pj * bf16_bits_to_f32((uint16_t)(u[r >> 1] >> (16 * (r & 1)))) : 0.f;
+                }
+            }
+          }
+        }
+        if (kt + 1 < kt1) arrive(cur ^ 1);
+        __syncthreads();
+      }
+    }
+
+    // ---- the job's result, or its part
+    l += __shfl_xor(l, 32, 64);
+    const bool whole = part.u0 == 0 && part.u1 == part.units;
+    const int64_t slot = 2 * worker + (part.u0 == 0 ? 1 : 0);
+    int x = wave * 32 + lq;
+    asm volatile("" : "+v"(x));  // (the row's place is formed again here, not kept over the loop)
+    x += p.tile * TR;
+    const bool valid = x < rows;
+    const int token = valid ? (int)div_by(x, a.by_rep) : 0, head = p.head * a.rep + (valid ? x - token * a.rep : 0);
+    if (valid && whole) {
+      const float inv = l != 0.f ? 1.f / l : 0.f;
+      uint16_t* op = static_cast<uint16_t*>(a.out) + (int64_t)(q.row0 + token) * a.out_stride + (int64_t)head * DH;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4)
+          *reinterpret_cast<uint2*>(op + nt * 32 + 2 * e + 4 * g) =
+              make_uint2(pack_bf16x2(acc[nt][e] * inv, acc[nt][e + 1] * inv), pack_bf16x2(acc[nt][e + 2] * inv, acc[nt][e + 3] * inv));
+      if (g == 0 && a.lse) a.lse[(int64_t)(q.row0 + token) * a.n_q_heads + head] = 0.6931471805599453f * (m + log2f(l));
+    } else if (valid) {
+      const int row = wave * 32 + lq;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4)
+          *reinterpret_cast<f32x4*>(a.part_o + ((slot * (DH / 4) + ((nt * 32 + 2 * e + 4 * g) >> 2)) * TR + row) * 4) =
+              f32x4{acc[nt][e], acc[nt][e + 1], acc[nt][e + 2], acc[nt][e + 3]};
+      if (g == 0) {
+        a.part_ml[slot * 2 * TR + row] = m;
+        a.part_ml[(slot * 2 + 1) * TR + row] = l;
+      }
+    }
+    if (tid == 0 && part.u0 == 0 && !whole)
+      a.rec[worker] = PagedRecord{paged_worker_of(part.last, p.total), q.row0, p.tile * TR, min(TR, rows - p.tile * TR), p.head};
+    at += part.steps;
+    if (at >= p.end) break;
+    paged_next<TR>(a, p, q);
+  }
+}
+
+template <int DH>
+void launch_many(const PagedArgs& a, hipStream_t s) {
+  static std::atomic<uint64_t> done[3];
+  const int f = a.c.format == KEEP_CACHE_BF16 ? 0 : a.c.format == KEEP_CACHE_FP8 ? 1 : 2;
+  const auto kernel = f == 0 ? k_paged_many<DH, KEEP_CACHE_BF16> : f == 1 ? k_paged_many<DH, KEEP_CACHE_FP8> : k_paged_many<DH, KEEP_CACHE_INT8>;
+  constexpr int bytes = Many<DH, KEEP_CACHE_BF16>::LDS;
+  set_max_dyn_smem_once(done[f], reinterpret_cast<const void*>(kernel), bytes);
+  hipLaunchKernelGGL(kernel, dim3(PAGED_WORKERS), dim3(256), (size_t)bytes, s, a);
+}
+
 template <int DH, int FMT, int RB>
 void launch_few(const PagedArgs& a, hipStream_t s) {
   static std::atomic<uint64_t> done{0};
@@ -427,8 +766,10 @@ void launch_few_format(const PagedArgs& a, hipStream_t s) {
 
 }  // namespace
 
-void launch_paged_few(const PagedArgs& a, int rows, hipStream_t s) {
-  if (a.c.head_dim == 128)
+void launch_paged_mfma(const PagedArgs& a, int rows, hipStream_t s) {
+  if (rows == MT_ROWS)
+    a.c.head_dim == 128 ? launch_many<128>(a, s) : launch_many<64>(a, s);
+  else if (a.c.head_dim == 128)
     rows == 16 ? launch_few_format<128, 1>(a, s) : launch_few_format<128, 2>(a, s);
   else
     rows == 16 ? launch_few_format<64, 1>(a, s) : launch_few_format<64, 2>(a, s);
