@@ -16,6 +16,8 @@
 // next arrives while one is used), where the matrix instruction and the exponentials are the bound.  32x32x16: a lane owns a
 // query row (lane % 32) and half of the tile's keys, and again S^T = K . Q^T leaves the operand of O^T = V^T . P^T.
 // 8-bit codes become bf16 on their way into LDS, once for the four waves.
+#include <type_traits>
+
 #include "paged_attn.h"
 
 namespace keep {
@@ -217,7 +219,9 @@ __global__ void __launch_bounds__(256, 2) k_paged_few(PagedArgs a) {
         v_off = request_k(t);
         request_v(t);
       }
-      for (int t = 0; t < n; ++t) {
+      // One slice; MASKED: some row does not see some key of it
+      const auto slice = [&](int t, auto masked_type) __attribute__((always_inline)) {
+        constexpr bool MASKED = decltype(masked_type)::value;
         const int slot = t % NS, kb = key0 + t * UNIT, left = min(NS - 1, n - 1 - t);
         const char* sk = ring + slot * F::BYTES;
         const char* sv = ring + (NS + slot) * F::BYTES;
@@ -267,7 +271,6 @@ __global__ void __launch_bounds__(256, 2) k_paged_few(PagedArgs a) {
         if (t + NS < n) v_off = request_k(t + NS);
 
         // ---- scores in the log2 domain, running maximum and sum
-        const bool masked = kb + SLICE - 1 > min_pos || kb < max_lo;
         bf16x8 pf[RB];
         float pr[RB][8];
 #pragma unroll
@@ -280,7 +283,7 @@ __global__ void __launch_bounds__(256, 2) k_paged_few(PagedArgs a) {
               v *= a.scale_log2e;
             else
               v *= k_sc[e >> 2][e & 3];
-            if (masked) {
+            if constexpr (MASKED) {
               const int key = kb + (e >> 2) * 16 + 4 * g + (e & 3);
               v = key <= pos[b] && key >= lo[b] ? v : -INFINITY;
             }
@@ -303,8 +306,8 @@ __global__ void __launch_bounds__(256, 2) k_paged_few(PagedArgs a) {
             if constexpr (!F::WIDE) {
               const float v0 = v_sc[e >> 2][e & 3], v1 = v_sc[e >> 2][(e & 3) + 1];
               // (a scale of NaN must not reach rows that do not see the key)
-              p0 = masked && pr[b][e] == -INFINITY ? 0.f : p0 * v0;
-              p1 = masked && pr[b][e + 1] == -INFINITY ? 0.f : p1 * v1;
+              p0 = MASKED && pr[b][e] == -INFINITY ? 0.f : p0 * v0;
+              p1 = MASKED && pr[b][e + 1] == -INFINITY ? 0.f : p1 * v1;
             }
             pr[b][e] = p0, pr[b][e + 1] = p1;
             pk[e >> 1] = pack_bf16x2(p0, p1);
@@ -324,9 +327,10 @@ __global__ void __launch_bounds__(256, 2) k_paged_few(PagedArgs a) {
           }
         }
         bool odd = false;
-        if (masked && FMT != KEEP_CACHE_INT8) {
+        if constexpr (MASKED && FMT != KEEP_CACHE_INT8) {
           // A product with a probability of zero would carry infinities and NaN to rows that do not see the key.
           constexpr uint32_t EXP = F::WIDE ? 0x7f807f80u : 0x7f7f7f7fu;
+#pragma unroll 2
           for (int i = lane; i < F::BYTES / 16; i += 64) {
             const u32x4 w = *reinterpret_cast<const u32x4*>(sv + i * 16);
 #pragma unroll
@@ -386,11 +390,18 @@ __global__ void __launch_bounds__(256, 2) k_paged_few(PagedArgs a) {
               for (int b = 0; b < RB; ++b)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) acc[b][i][r] += key <= pos[b] && key >= lo[b] ? pj[b] * v[r] : 0.f;
+              __builtin_amdgcn_sched_barrier(0);  // (one read at a time: this path must not cost the others registers)
             }
           }
         }
         lds_wait();
         if (t + NS < n) request_v(t + NS);
+      };
+      // Two loops, so that what masks need takes no registers from the slices without: they are nearly all of them
+      const auto is_masked = [&](int t) { return key0 + t * UNIT + SLICE - 1 > min_pos || key0 + t * UNIT < max_lo; };
+      for (int t = 0; t < n;) {
+        for (; t < n && !is_masked(t); ++t) slice(t, std::false_type{});
+        for (; t < n && is_masked(t); ++t) slice(t, std::true_type{});
       }
     }
 
@@ -466,13 +477,14 @@ __global__ void __launch_bounds__(256, 2) k_paged_many(PagedArgs a) {
     // ---- this lane's query row, and what the wave's rows see: keys up to pos, from lo on
     const int rows = q.rows * a.rep;
     int pos, lo;
-    int max_pos = -1, min_pos = -1, max_lo = 0, min_lo = 0;
+    // the wave's last key and first one, and the keys that every row of the tile sees (lanes without a row are not stored)
+    int max_pos = -1, min_lo = 0;
+    const int min_pos = q.len - q.rows + (int)div_by(p.tile * TR, a.by_rep);
+    const int max_lo = a.window ? max(0, q.len - q.rows + (int)div_by(min(rows, (p.tile + 1) * TR) - 1, a.by_rep) - a.window + 1) : 0;
     {
       const int x0 = p.tile * TR + wave * 32, x1 = min(rows, x0 + 32) - 1;
       if (x0 < rows) {
-        min_pos = x1 - x0 < 31 ? -1 : q.len - q.rows + (int)div_by(x0, a.by_rep);  // (lanes without a row see nothing)
         max_pos = q.len - q.rows + (int)div_by(x1, a.by_rep);
-        max_lo = a.window ? max(0, max_pos - a.window + 1) : 0;
         min_lo = a.window ? max(0, q.len - q.rows + (int)div_by(x0, a.by_rep) - a.window + 1) : 0;
       }
     }
@@ -510,40 +522,49 @@ __global__ void __launch_bounds__(256, 2) k_paged_many(PagedArgs a) {
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[ks]));  // (in registers before the tiles' loads begin)
 
-      // ---- tile kt to buffer `buf`.  bf16: straight to LDS, a wave 16 rows of it.  8 bits: 16 codes of a row per load, kept in
-      // registers until the other buffer has been used.  Keys past the end read the last one again and are masked.
-      constexpr int LPR = DH / 16, RPL = 256 / LPR, NL = KT / RPL;  // 8 bits: threads per row, rows of a load, loads
+      // ---- tile kt to buffer `buf`.  bf16: straight to LDS.  8 bits: 16 codes of a row per load, kept in registers until the
+      // other buffer has been used.  A wave loads 16 rows of a tile, RW per load with LPR lanes each.  Keys past the end read the
+      // last one again and are masked.
+      constexpr int LPR = DH * (F::WIDE ? 2 : 1) / 16, RW = 64 / LPR, NL = 16 / RW;
+      const auto row_of = [&](int j) { return F::WIDE ? wave * 16 + j : j / RW * (4 * RW) + wave * RW + j % RW; };
       u32x4 kc[F::WIDE ? 1 : NL], vc[F::WIDE ? 1 : NL];
       float sc = 0.f;
-      const auto place = [&](int key, int64_t& scale) {
-        const int n = (int)div_by(key, a.by_page), in = key - n * a.c.page_size, page = tbl[n - page0];
-        scale = ((int64_t)page * a.c.n_kv_heads + p.head) * a.c.page_size + in;
-        return page * a.c.page_stride + in * a.c.token_stride + head_at;
+      const int last = max(q.len, 1) - 1;
+      const auto find = [&](int key, int& page, int& in) {
+        const int n = (int)div_by(min(key, last), a.by_page);
+        in = min(key, last) - n * a.c.page_size;
+        page = tbl[n - page0];
       };
-      const auto request = [&](int kt, int buf) {
-        const int last = max(q.len, 1) - 1;
-        int64_t s;
-        if constexpr (F::WIDE) {
-          constexpr int PER = 64 / CH, NI = 16 / PER;  // rows of a load, loads of a wave's 16 rows
+      // Where row lane % 16 of this wave's share of tile kt lies, in 16 bytes: formed a tile ahead of its loads
+      const auto locate = [&](int kt) {
+        int page, in, ln = lane;
+        asm volatile("" : "+v"(ln));
+        find(kt * KT + row_of(ln & 15), page, in);
+        return (uint32_t)((page * a.c.page_stride + in * a.c.token_stride + head_at) * (F::WIDE ? 2 : 1) / 16);
+      };
+      const auto request = [&](int kt, int buf, uint32_t where) {
+        int ln = lane;
+        asm volatile("" : "+v"(ln));  // (what follows from the lane is formed anew: kept, it would push registers out to memory)
 #pragma unroll
-          for (int i = 0; i < NI; ++i) {
-            const int row = wave * 16 + i * PER + lane / CH;
-            const int64_t e = place(min(kt * KT + row, last), s);
-            const uint32_t to = lds_at + buf * 2 * F::TILE + (wave * 16 + i * PER) * ROW;
-            load_lds16(static_cast<const __bf16*>(a.c.k) + e + mk_chunk<CH>(row, lane % CH) * 8, to);
-            load_lds16(static_cast<const __bf16*>(a.c.v) + e + mv_chunk<CH>(row, lane % CH) * 8, to + F::TILE);
+        for (int i = 0; i < NL; ++i) {
+          const int row = row_of(i * RW + ln / LPR);
+          const int64_t e = (int64_t)(uint32_t)__shfl((int)where, i * RW + ln / LPR, 64) * 16;
+          const char* k = static_cast<const char*>(a.c.k) + e;
+          const char* v = static_cast<const char*>(a.c.v) + e;
+          if constexpr (F::WIDE) {
+            const uint32_t to = lds_at + buf * 2 * F::TILE + (wave * 16 + i * RW) * ROW;
+            load_lds16(k + mk_chunk<CH>(row, ln % CH) * 16, to);
+            load_lds16(v + mv_chunk<CH>(row, ln % CH) * 16, to + F::TILE);
+          } else {
+            kc[i] = *reinterpret_cast<const u32x4*>(k + (ln % LPR) * 16);
+            vc[i] = *reinterpret_cast<const u32x4*>(v + (ln % LPR) * 16);
           }
-        } else {
-#pragma unroll
-          for (int i = 0; i < NL; ++i) {
-            const int64_t e = place(min(kt * KT + i * RPL + tid / LPR, last), s) + (tid % LPR) * 16;
-            kc[i] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(a.c.k) + e);
-            vc[i] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(a.c.v) + e);
-          }
-          if (tid < 2 * KT) {
-            place(min(kt * KT + (tid & (KT - 1)), last), s);
-            sc = tid < KT ? a.c.k_scale[s] * a.scale_log2e : a.c.v_scale[s];
-          }
+        }
+        if (!F::WIDE && tid < 2 * KT) {
+          int page, in;
+          find(kt * KT + (tid & (KT - 1)), page, in);
+          const int64_t s = ((int64_t)page * a.c.n_kv_heads + p.head) * a.c.page_size + in;
+          sc = tid < KT ? a.c.k_scale[s] * a.scale_log2e : a.c.v_scale[s];
         }
       };
       const auto arrive = [&](int buf) {
@@ -551,9 +572,11 @@ __global__ void __launch_bounds__(256, 2) k_paged_many(PagedArgs a) {
           vm_wait<0>();
         } else {
           char* to = lds + buf * 2 * F::TILE;
+          int ln = lane;
+          asm volatile("" : "+v"(ln));
 #pragma unroll
           for (int i = 0; i < NL; ++i) {
-            const int row = i * RPL + tid / LPR, c = 2 * (tid % LPR);
+            const int row = row_of(i * RW + ln / LPR), c = 2 * (ln % LPR);
             *reinterpret_cast<bf16x8*>(to + row * ROW + mk_chunk<CH>(row, c) * 16) = codes8<FMT>(kc[i][0], kc[i][1]);
             *reinterpret_cast<bf16x8*>(to + row * ROW + mk_chunk<CH>(row, c + 1) * 16) = codes8<FMT>(kc[i][2], kc[i][3]);
             *reinterpret_cast<bf16x8*>(to + F::TILE + row * ROW + mv_chunk<CH>(row, c) * 16) = codes8<FMT>(vc[i][0], vc[i][1]);
@@ -563,28 +586,52 @@ __global__ void __launch_bounds__(256, 2) k_paged_many(PagedArgs a) {
         }
       };
 
-      request(kt0, 0);
+      request(kt0, 0, locate(kt0));
+      uint32_t where = locate(min(kt0 + 1, kt1 - 1));
       arrive(0);
       __syncthreads();
-      for (int kt = kt0; kt < kt1; ++kt) {
+      // One tile; MASKED: some row of the workgroup does not see some key of it
+      const auto tile = [&](int kt, auto masked_type) __attribute__((always_inline)) {
+        constexpr bool MASKED = decltype(masked_type)::value;
         const int cur = (kt - kt0) & 1, k0 = kt * KT;
         // every wave finished reading the other buffer before the barrier that ended the last iteration
-        if (kt + 1 < kt1) request(kt + 1, cur ^ 1);
-        if (k0 <= max_pos && k0 + KT > min_lo) {
+        if (kt + 1 < kt1) {
+          request(kt + 1, cur ^ 1, where);
+          where = locate(min(kt + 2, kt1 - 1));
+        }
+        if (!MASKED || (k0 <= max_pos && k0 + KT > min_lo)) {
           const char* sk = lds + cur * 2 * F::TILE;
           const char* sv = sk + F::TILE;
           const float* ksc = scales + cur * 2 * KT;
           int k_at = k_first, v_at = v_first;
           asm volatile("" : "+v"(k_at), "+v"(v_at));
+          // S^T for the two halves of the keys; K operands are read four steps ahead, the first V operands before the softmax
           f32x16 s[2];
+          bf16x8 kf[2 * KS];
+          const auto read_k = [&](int from) {
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
+            for (int i = from; i < from + 4; ++i)
+              if (i < 2 * KS) kf[i] = *reinterpret_cast<const bf16x8*>(sk + i / KS * 32 * ROW + (k_at ^ (i % KS * 32)));
+          };
+          s16x4 vf[2][NT][2];
+          const auto read_v = [&](int step) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int b = 0; b < 2; ++b)
+                vf[step & 1][nt][b] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(sv + (step * 16 + b * 8) * ROW + (v_at ^ (nt * 64))));
+          };
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[h][e] = 0.f;
+          read_k(0);
+          read_k(4);
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
-              s[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(sk + h * 32 * ROW + (k_at ^ (ks * 32))), qf[ks],
-                                                             s[h], 0, 0, 0);
+          for (int i = 0; i < 2 * KS; ++i) {
+            s[i / KS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], qf[i % KS], s[i / KS], 0, 0, 0);
+            if (i % 4 == 3) read_k(i + 5);
+            if (i == 2 * KS - 5) read_v(0);
           }
           // ---- scores (8 bits: in the log2 domain already), mask, running maximum
           if constexpr (!F::WIDE) {
@@ -597,8 +644,7 @@ __global__ void __launch_bounds__(256, 2) k_paged_many(PagedArgs a) {
                 for (int e = 0; e < 4; ++e) s[h][4 * i + e] *= f[e];
               }
           }
-          const bool masked = k0 + KT - 1 > min_pos || k0 < max_lo;
-          if (masked) {
+          if constexpr (MASKED) {
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -637,14 +683,15 @@ __global__ void __launch_bounds__(256, 2) k_paged_many(PagedArgs a) {
               l += p0 + p1;
               if constexpr (!F::WIDE) {
                 const float* v = ksc + KT + h * 32 + 8 * (e >> 2) + 4 * g + (e & 3);
-                p0 = masked && s[h][e] == -INFINITY ? 0.f : p0 * v[0];  // (a scale of NaN stays with the rows that see the key)
-                p1 = masked && s[h][e + 1] == -INFINITY ? 0.f : p1 * v[1];
+                p0 = MASKED && s[h][e] == -INFINITY ? 0.f : p0 * v[0];  // (a scale of NaN stays with the rows that see the key)
+                p1 = MASKED && s[h][e + 1] == -INFINITY ? 0.f : p1 * v[1];
               }
               pk[h][e >> 1] = pack_bf16x2(p0, p1);
             }
           bool odd = false;
-          if (masked && FMT != KEEP_CACHE_INT8) {
+          if constexpr (MASKED && FMT != KEEP_CACHE_INT8) {
             // A product with a probability of zero would carry infinities and NaN to rows that do not see the key.
+#pragma unroll 2
             for (int i = lane; i < F::TILE / 16; i += 64) {
               const u32x4 w = *reinterpret_cast<const u32x4*>(sv + i * 16);
 #pragma unroll
@@ -656,18 +703,16 @@ __global__ void __launch_bounds__(256, 2) k_paged_many(PagedArgs a) {
             // slot (g, i) of step s holds key 16 s + 8 (i / 4) + 4 g + i % 4: the keys of P^T's registers as they are
 #pragma unroll
             for (int step = 0; step < 4; ++step) {
+              if (step + 1 < 4) read_v(step + 1);
               u32x4 pu;
 #pragma unroll
               for (int i = 0; i < 4; ++i) pu[i] = pk[step >> 1][(step & 1) * 4 + i];
               const bf16x8 pf = __builtin_bit_cast(bf16x8, pu);
-              const char* vb = sv + step * 16 * ROW;
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt) {
-                const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(vb + (v_at ^ (nt * 64))));
-                const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(vb + 8 * ROW + (v_at ^ (nt * 64))));
+              for (int nt = 0; nt < NT; ++nt)
                 acc[nt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                    __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7)), pf, acc[nt], 0, 0, 0);
-              }
+                    __builtin_bit_cast(bf16x8, __builtin_shufflevector(vf[step & 1][nt][0], vf[step & 1][nt][1], 0, 1, 2, 3, 4, 5, 6, 7)),
+                    pf, acc[nt], 0, 0, 0);
             }
           } else {
 #pragma unroll 1
@@ -688,12 +733,19 @@ __global__ void __launch_bounds__(256, 2) k_paged_many(PagedArgs a) {
 #pragma unroll
                   for (int r = 0; r < 4; ++r)
                     acc[nt][4 * i + r] += sees ? pj * bf16_bits_to_f32((uint16_t)(u[r >> 1] >> (16 * (r & 1)))) : 0.f;
+                  __builtin_amdgcn_sched_barrier(0);  // (one read at a time: this path must not cost the others registers)
                 }
             }
           }
         }
         if (kt + 1 < kt1) arrive(cur ^ 1);
         __syncthreads();
+      };
+      // Two loops, so that what masks need takes no registers from the tiles without: they are nearly all of them
+      const auto is_masked = [&](int kt) { return kt * KT + KT - 1 > min_pos || kt * KT < max_lo; };
+      for (int kt = kt0; kt < kt1;) {
+        for (; kt < kt1 && !is_masked(kt); ++kt) tile(kt, std::false_type{});
+        for (; kt < kt1 && is_masked(kt); ++kt) tile(kt, std::true_type{});
       }
     }
 
