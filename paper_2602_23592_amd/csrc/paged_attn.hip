@@ -177,25 +177,49 @@ __global__ void __launch_bounds__(256) k_paged_generic(PagedArgs a) {
   }
 }
 
-// The parts of a job that was cut, joined in the order of their keys.  A workgroup takes the job that worker blockIdx.x left a
-// record of, each of its eight waves 16 of the output's dimensions at a time.  Lanes lie along query rows and then along
-// parts, each with a running maximum and sum of its own, so that all loads are independent of one another; a butterfly adds the
-// lanes of a row.  (Most workgroups find no record, so few and large ones: 64 parts of 5 rows, 8 such jobs took 12 us
-// with a workgroup per 16 dimensions.)
+// The parts of a job that was cut, joined in the order of their keys.  Workgroup x takes the x-th job that a worker left a record
+// of, and `groups` times 16 of the output's dimensions (blockIdx.y).  Lanes lie along query rows, then along parts, and as many
+// waves as there are to spare for 16 dimensions along parts again, each lane with a running maximum and sum of its own, so that all
+// loads are independent of one another; a butterfly adds the lanes of a row, LDS the waves.
+// (8 jobs of 64 parts of 5 rows: 21 us with the parts along 8 lanes and two passes over them, 12 with 4096 workgroups of
+// which nearly all find no record, 7 with a wave for all of a job's parts, 4 like this.)
 template <int TR>
-__global__ void __launch_bounds__(512) k_paged_join(PagedArgs a) {
+__global__ void __launch_bounds__(512) k_paged_join(PagedArgs a, int groups) {
   constexpr int RB = TR < 64 ? TR : 64;  // rows side by side in a wave
-  const PagedRecord r = a.rec[blockIdx.x];
-  if (r.last == 0) return;
-  const int quads = a.c.head_dim / 4, n = r.last - (int)blockIdx.x + 1, w0 = blockIdx.x;
-  const int lane = threadIdx.x & 63;
-  int rb = 1;
+  __shared__ float s_m[8][RB], s_l[8][RB];
+  __shared__ f32x4 s_o[8][4][RB];
+  __shared__ int s_count[8], s_w0;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (gridDim.x == PAGED_WORKERS) {  // a workgroup for every worker: no need to count
+    if (a.rec[blockIdx.x].last == 0) return;
+    if (threadIdx.x == 0) s_w0 = blockIdx.x;
+    __syncthreads();
+  } else {
+    static_assert(PAGED_WORKERS == 512, "a thread looks at one record");
+    const bool is = a.rec[threadIdx.x].last != 0;
+    const uint64_t some = __ballot(is);
+    if (lane == 0) s_count[wave] = __popcll(some);
+    if (threadIdx.x == 0) s_w0 = -1;
+    __syncthreads();
+    int rank = __popcll(some & ((1ull << lane) - 1));
+    for (int w = 0; w < wave; ++w) rank += s_count[w];
+    if (is && rank == (int)blockIdx.x) s_w0 = threadIdx.x;
+    __syncthreads();
+  }
+  const int w0 = s_w0;
+  if (w0 < 0) return;
+  const PagedRecord r = a.rec[w0];
+  const int quads = a.c.head_dim / 4, n = r.last - w0 + 1;
+  int rb = 1, along = 1;  // rows in a wave; waves along the parts
   while (rb < min(r.n, RB)) rb *= 2;
-  const int part0 = lane / rb, step = 64 / rb;
-  for (int q0 = (threadIdx.x >> 6) * 4; q0 < quads; q0 += 32)
+  while (2 * along * groups <= 8) along *= 2;
+  const int lanes = 64 / rb, part0 = (wave & (along - 1)) * lanes + lane / rb, step = along * lanes;
+  for (int g0 = 0; g0 < groups; g0 += 8 / along) {
+    const int q0 = ((int)blockIdx.y * groups + g0 + wave / along) * 4;
+    const bool dims = g0 + wave / along < groups && q0 < quads;
     for (int base = 0; base < r.n; base += rb) {
       const int row = base + (lane & (rb - 1));
-      const bool valid = row < r.n;
+      const bool valid = dims && row < r.n;
       float m = -INFINITY, l = 0.f;
       f32x4 o[4] = {};
       if (valid) {
@@ -227,6 +251,26 @@ __global__ void __launch_bounds__(512) k_paged_join(PagedArgs a) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) o[j][e] += __shfl_xor(o[j][e], s, 64);
       }
+      if (along > 1) {
+        __syncthreads();  // (the sums before have been read)
+        if (lane < rb) {
+          s_m[wave][lane] = m, s_l[wave][lane] = l;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s_o[wave][j][lane] = o[j];
+        }
+        __syncthreads();
+        if ((wave & (along - 1)) != 0 || lane >= rb) continue;
+        for (int w = wave; w < wave + along; ++w) m = fmaxf(m, s_m[w][lane]);
+        l = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int w = wave; w < wave + along; ++w) {
+          const float f = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(s_m[w][lane] - m);
+          l += s_l[w][lane] * f;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[j] += f == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : s_o[w][j][lane] * f;
+        }
+      }
       if (!valid || lane >= rb) continue;
       const int x = r.x0 + row, token = (int)div_by(x, a.by_rep), head = r.head * a.rep + x - token * a.rep;
       const int64_t o_at = (int64_t)(r.row0 + token) * a.out_stride + (int64_t)head * a.c.head_dim + q0 * 4;
@@ -241,6 +285,7 @@ __global__ void __launch_bounds__(512) k_paged_join(PagedArgs a) {
       }
       if (q0 == 0 && a.lse) a.lse[(int64_t)(r.row0 + token) * a.n_q_heads + head] = 0.6931471805599453f * (m + log2f(l));
     }
+  }
 }
 
 uint64_t part_bytes(int tr, int dh) { return (uint64_t)2 * PAGED_WORKERS * tr * (dh + 2) * sizeof(float); }
@@ -267,8 +312,12 @@ void launch_paged_generic(const PagedArgs& a, hipStream_t s) {
 }
 
 void launch_paged_join(const PagedArgs& a, int rows, hipStream_t s) {
+  // no more jobs than tiles, and few workgroups share the dimensions of few jobs
+  const int64_t tiles = (a.n_rows * (int64_t)a.rep / rows + a.n_seqs) * a.c.n_kv_heads;
+  const int jobs = (int)std::min<int64_t>(PAGED_WORKERS, tiles), all = a.c.head_dim / 16;
+  const int groups = (all + std::max(1, 256 / jobs) - 1) / std::max(1, 256 / jobs);
   const auto kernel = rows == 16 ? k_paged_join<16> : rows == 32 ? k_paged_join<32> : k_paged_join<128>;
-  hipLaunchKernelGGL(kernel, dim3(PAGED_WORKERS), dim3(512), 0, s, a);
+  hipLaunchKernelGGL(kernel, dim3(jobs, (all + groups - 1) / groups), dim3(512), 0, s, a, groups);
 }
 
 }  // namespace keep
@@ -340,11 +389,13 @@ extern "C" keep_status keep_paged_attention(const keep_paged_attention_desc* d, 
   a.rec = reinterpret_cast<PagedRecord*>(ws);
   a.part_ml = reinterpret_cast<float*>(ws + REC_BYTES);
   if (!format_scaled(cache->format)) a.c.k_scale = a.c.v_scale = nullptr;
-  // The bf16 matrix instruction where it has a kernel.  Tiles of 16 query rows while sequences bring no more on average (one to a
-  // few tokens), then of 32, then of 128.
+  // The bf16 matrix instruction where it has a kernel, in tiles of 16, 32 or 128 query rows by what a sequence brings on average.
+  // us on tiles of 16 / 32 / 128 for 30, 60 and 125 rows per sequence, 64 ragged sequences of up to 8k keys in bf16: 331 / 213 /
+  // 260, 629 / 351 / 284, 1207 / 671 / 303 (fp8: 184 / 143 / 237, 340 / 233 / 260); one sequence of 33k keys: 55 / 50 / 58,
+  // 59 / 56 / 64, 89 / 67 / 75.  Up to 16 rows a tile of 32 has nothing to gain.
   const bool mfma = d->dtype == KEEP_BF16 && has_mfma(cache);
   const int64_t mean = (d->n_rows * (int64_t)a.rep + d->n_seqs - 1) / d->n_seqs;
-  const int rows = !mfma || mean <= 16 ? 16 : mean <= 32 ? 32 : 128;
+  const int rows = !mfma || mean <= 16 ? 16 : mean <= 48 ? 32 : 128;
   a.part_o = a.part_ml + (size_t)2 * PAGED_WORKERS * 2 * rows;
   if (mfma)
     launch_paged_mfma(a, rows, static_cast<hipStream_t>(stream));

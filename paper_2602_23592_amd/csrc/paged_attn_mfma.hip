@@ -189,28 +189,33 @@ __global__ void __launch_bounds__(256, 2) k_paged_few(PagedArgs a) {
       const int key0 = (first + ub) * UNIT + wave * SLICE;
       const int n = key0 > max_pos ? 0 : min(ue - ub, (max_pos - key0) / UNIT + 1);
       uint32_t v_off = 0;  // per lane: where key lane % 32 of the youngest requested slice lies, in 16 bytes
+      // (What follows from the lane is formed anew in every slice: kept, it would push registers out to memory.)
       const auto request_k = [&](int t) {
-        const int key = min(key0 + t * UNIT + (lane & 31), q.len - 1), pg = (int)div_by(key, a.by_page);
+        int ln = lane;
+        asm volatile("" : "+v"(ln));
+        const int key = min(key0 + t * UNIT + (ln & 31), q.len - 1), pg = (int)div_by(key, a.by_page);
         const int page = tbl[pg - page0], in = key - pg * a.c.page_size;
         const uint32_t off = (uint32_t)((page * a.c.page_stride + in * a.c.token_stride) * (F::WIDE ? 2 : 1) / 16);
         const int slot = t % NS;
         if constexpr (!F::WIDE)
-          load_lds4((lane < 32 ? a.c.k_scale : a.c.v_scale) + ((int64_t)page * a.c.n_kv_heads + p.head) * a.c.page_size + in,
+          load_lds4((ln < 32 ? a.c.k_scale : a.c.v_scale) + ((int64_t)page * a.c.n_kv_heads + p.head) * a.c.page_size + in,
                     ring_at + 2 * NS * F::BYTES + slot * 256);
 #pragma unroll
         for (int i = 0; i < F::NI; ++i) {
-          const int row = i * F::PER + lane / CH;
-          load_lds16(k_base + head_at + (int64_t)(uint32_t)__shfl((int)off, row, 64) * 16 + k_chunk<CH>(row, lane % CH) * 16,
+          const int row = i * F::PER + ln / CH;
+          load_lds16(k_base + head_at + (int64_t)(uint32_t)__shfl((int)off, row, 64) * 16 + k_chunk<CH>(row, ln % CH) * 16,
                      ring_at + slot * F::BYTES + i * 1024);
         }
         return off;
       };
       const auto request_v = [&](int t) {
         const int slot = t % NS;
+        int ln = lane;
+        asm volatile("" : "+v"(ln));
 #pragma unroll
         for (int i = 0; i < F::NI; ++i) {
-          const int row = i * F::PER + lane / CH;
-          load_lds16(v_base + head_at + (int64_t)(uint32_t)__shfl((int)v_off, row, 64) * 16 + v_chunk<CH, F::WIDE>(row, lane % CH) * 16,
+          const int row = i * F::PER + ln / CH;
+          load_lds16(v_base + head_at + (int64_t)(uint32_t)__shfl((int)v_off, row, 64) * 16 + v_chunk<CH, F::WIDE>(row, ln % CH) * 16,
                      ring_at + (NS + slot) * F::BYTES + i * 1024);
         }
       };
@@ -223,6 +228,9 @@ __global__ void __launch_bounds__(256, 2) k_paged_few(PagedArgs a) {
       const auto slice = [&](int t, auto masked_type) __attribute__((always_inline)) {
         constexpr bool MASKED = decltype(masked_type)::value;
         const int slot = t % NS, kb = key0 + t * UNIT, left = min(NS - 1, n - 1 - t);
+        int ln = lane;
+        asm volatile("" : "+v"(ln));
+        const int col = ln & 15, g = ln >> 4;
         const char* sk = ring + slot * F::BYTES;
         const char* sv = ring + (NS + slot) * F::BYTES;
         const float* scales = reinterpret_cast<const float*>(ring + 2 * NS * F::BYTES + slot * 256);
@@ -605,7 +613,8 @@ __global__ void __launch_bounds__(256, 2) k_paged_many(PagedArgs a) {
           const float* ksc = scales + cur * 2 * KT;
           int k_at = k_first, v_at = v_first;
           asm volatile("" : "+v"(k_at), "+v"(v_at));
-          // S^T for the two halves of the keys; K operands are read four steps ahead, the first V operands before the softmax
+          // S^T for the two halves of the keys; K operands are read four steps ahead, the first V operands before the softmax (8
+          // bits: the next tile's codes take the registers for that)
           f32x16 s[2];
           bf16x8 kf[2 * KS];
           const auto read_k = [&](int from) {
@@ -631,7 +640,7 @@ __global__ void __launch_bounds__(256, 2) k_paged_many(PagedArgs a) {
           for (int i = 0; i < 2 * KS; ++i) {
             s[i / KS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], qf[i % KS], s[i / KS], 0, 0, 0);
             if (i % 4 == 3) read_k(i + 5);
-            if (i == 2 * KS - 5) read_v(0);
+            if (F::WIDE && i == 2 * KS - 5) read_v(0);
           }
           // ---- scores (8 bits: in the log2 domain already), mask, running maximum
           if constexpr (!F::WIDE) {
@@ -701,6 +710,7 @@ __global__ void __launch_bounds__(256, 2) k_paged_many(PagedArgs a) {
           }
           if (!odd) {
             // slot (g, i) of step s holds key 16 s + 8 (i / 4) + 4 g + i % 4: the keys of P^T's registers as they are
+            if (!F::WIDE) read_v(0);
 #pragma unroll
             for (int step = 0; step < 4; ++step) {
               if (step + 1 < 4) read_v(step + 1);
