@@ -175,7 +175,7 @@ uint64_t keep_sample_workspace_bytes(int32_t n_rows, int32_t vocab);
 
 /*   logits: DEVICE, element-aligned.  uniform: DEVICE float [n_rows], clamped to [0, 1).
  *   temperature, top_k, top_p, min_p: DEVICE [n_rows] each (float, int32, float, float), or NULL: 1, no limits.  top_k < 1,
- *     top_p NaN and min_p <= 0 or NaN are no limits; top_p <= 0 keeps the likeliest token, min_p > 1 counts as 1.
+ *     top_p >= 1 or NaN and min_p <= 0 or NaN are no limits; top_p <= 0 keeps the likeliest token, min_p > 1 counts as 1.
  *   tokens: DEVICE int32 [n_rows].  probs: DEVICE float [n_rows] or NULL: the token's share of what stayed.
  *   workspace: DEVICE, 256-byte aligned, at least keep_sample_workspace_bytes.
  * Errors: INVALID_ARG, SHAPE (vocab), WORKSPACE, HIP. */

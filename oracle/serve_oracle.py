@@ -132,7 +132,7 @@ def sample(x, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
     rank = sorted((i for i in range(len(x)) if w[i] >= least), key=lambda i: (-x[i], i))
     if top_k >= 1:
         rank = rank[:top_k]
-    if not math.isnan(top_p):
+    if top_p < 1:
         goal = math.ceil(top_p * float(sum(w[i] for i in rank)))
         kept, mass = [], 0
         for i in rank:

@@ -93,6 +93,7 @@ struct keep_ctx {
   int32_t* d_dec = nullptr;         // device mirror
   float* dec_logits = nullptr;      // [vocab]
   uint64_t* argmax_part = nullptr;  // [ARGMAX_BLOCKS]
+  void* sample_ws = nullptr;        // workspace of the sampled choice
   float* h_S = nullptr;             // [(max_groups+1) * max_groups]
   int32_t* h_token_ids = nullptr;   // [max_tokens]
 
@@ -123,7 +124,8 @@ namespace {
 namespace keep {
 // sample.hip: one row of fp32 logits; how->uniform is not read (d_uniform: DEVICE), a row without a number gives token 0
 void launch_sample_decode(const float* logits, int32_t vocab, const float* d_uniform, const keep_sampling& how, int32_t* token,
-                          float* prob, hipStream_t s);
+                          float* prob, void* workspace /*[sample_decode_bytes()]*/, hipStream_t s);
+uint64_t sample_decode_bytes();
 // message behind keep_last_error(NULL), for entry points that have no context
 void set_init_error(const char* text) { g_init_error = text; }
 }  // namespace keep
@@ -258,7 +260,7 @@ uint64_t workspace_bytes(const keep_model_desc* d) {
   t += align256(select_scratch_words((int32_t)z.G) * sizeof(float));   // sel_scratch
   t += align256((z.G + 2) * sizeof(int32_t));                          // sel_out
   t += align256(6 * KEEP_DECODE_MAX_TOKENS * 4) + align256((size_t)d->vocab * sizeof(float));  // decode
-  t += align256(ARGMAX_BLOCKS * sizeof(uint64_t));
+  t += align256(ARGMAX_BLOCKS * sizeof(uint64_t)) + align256(sample_decode_bytes());
   t += 2 * align256(z.M * sizeof(int32_t));                            // row_lo, row_list
   t += 3 * align256(z.M * sizeof(int32_t));                            // token deviation, flags, kept list
   return t;
@@ -725,7 +727,8 @@ keep_status decode_impl(keep_ctx* c, const void* final_norm, const void* lm_head
     else
       launch_gemm_generic<T>(Typed<T>::p(c->hbuf), 1, d.hidden, bh, nullptr, d.vocab, EPI_STORE_F32, nullptr, lg, s);
     if (how)
-      launch_sample_decode(lg, d.vocab, d_float + 4 * CAP + t, *how, c->d_dec + 2 * CAP + t, d_float + 5 * CAP + t, s);
+      launch_sample_decode(lg, d.vocab, d_float + 4 * CAP + t, *how, c->d_dec + 2 * CAP + t, d_float + 5 * CAP + t,
+                           c->sample_ws, s);
     else
       launch_argmax(lg, d.vocab, c->d_dec + 2 * CAP + t, c->argmax_part, s);
     HIP_TRY(c, hipGetLastError());
@@ -1019,6 +1022,7 @@ keep_status keep_init(const keep_model_desc* desc, const keep_layer_weights* lay
   TRY_INIT(dev_alloc(c, &c->d_dec, 6 * KEEP_DECODE_MAX_TOKENS * 4));
   TRY_INIT(dev_alloc(c, &c->dec_logits, (size_t)desc->vocab * sizeof(float)));
   TRY_INIT(dev_alloc(c, &c->argmax_part, ARGMAX_BLOCKS * sizeof(uint64_t)));
+  TRY_INIT(dev_alloc(c, &c->sample_ws, sample_decode_bytes()));
   TRY_INIT(pin_alloc(c, &c->h_S, (z.G + 1) * z.G * sizeof(float)));
   TRY_INIT(pin_alloc(c, &c->h_token_ids, z.M * 4));
   auto mk_events = [&]() -> keep_status {

@@ -31,7 +31,7 @@ def fast(x, u, t, k, p, mp):
     ids = ids[np.lexsort((ids, -x[ids]))]
     ids = ids[:k] if k >= 1 else ids
     ends = np.cumsum(w[ids])
-    if not math.isnan(p):
+    if p < 1:
         ids = ids[:np.searchsorted(ends, max(1, math.ceil(p * float(int(ends[-1])))), side="left") + 1]
     ends = ends[:len(ids)]
     total = int(ends[-1])
