@@ -337,8 +337,13 @@ def _refuse(text: str):
 
 def _launch(device: torch.device, stream, call, *args):
     """One call on `stream`, by default the current one of the tensors' device, with that device current."""
-    with torch.cuda.device(device):
-        st = call(*args, _stream_handle(stream if stream is not None else torch.cuda.current_stream(device)))
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    if torch.cuda.current_device() == device.index:
+        st = call(*args, _stream_handle(stream))
+    else:
+        with torch.cuda.device(device):
+            st = call(*args, _stream_handle(stream))
     if st != KEEP_OK:
         raise KeepError(st, _lib.keep_last_error(None).decode())
 
@@ -347,19 +352,20 @@ def _array(name: str, t: Optional[torch.Tensor], dtype, numel: int, device: torc
     """Address of a dense device array of `numel` elements"""
     if t is None:
         return None if optional else _refuse(name + " is missing")
-    if t.dtype != dtype or t.numel() != numel or not t.is_contiguous() or t.device != device:
+    if t.dtype is not dtype or t.numel() != numel or not t.is_contiguous() or t.device != device:
         _refuse("%s must be a dense %s array of %d elements on %s" % (name, dtype, numel, device))
     return t.data_ptr()
 
 
 def _heads(name: str, t: torch.Tensor, device: torch.device, dtype=None) -> int:
     """Row stride of [rows, heads, head_dim] whose rows are dense"""
-    if t.dim() != 3 or t.device != device or t.dtype not in _DTYPES or (dtype is not None and t.dtype != dtype):
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or t.device != device or not (t.dtype is dtype if dtype is not None else t.dtype in _DTYPES):
         _refuse("%s must be [rows, heads, head_dim] in float32 or bfloat16, of one type and on one device" % name)
-    rows, h, d = t.shape
-    if not (t.numel() == 0 or ((d == 1 or t.stride(2) == 1) and (h == 1 or t.stride(1) == d))):
+    rows, h, d = shape
+    if not ((d <= 1 or stride[2] == 1) and (h <= 1 or stride[1] == d)) and rows * h * d:
         _refuse("the heads of a row of %s must be adjacent" % name)
-    return t.stride(0) if rows > 1 else h * d
+    return stride[0] if rows > 1 else h * d
 
 
 def rope_frequencies(rot_dim: int, theta: float = 1.0e6, scaling: int = KEEP_ROPE_PLAIN, factor: float = 1.0,
@@ -384,23 +390,26 @@ def rope_rows(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: t
     ref = q if q is not None else k
     if ref is None:
         _refuse("neither queries nor keys")
-    q_out, k_out = q if q_out is None else q_out, k if k_out is None else k_out
-    n, d = ref.shape[0], ref.shape[-1]
-    strides = []
-    for name, t in (("q", q), ("q_out", q_out), ("k", k), ("k_out", k_out)):
-        if t is None:
-            strides.append(0)
-            continue
-        strides.append(_heads(name, t, ref.device, ref.dtype))
-        if t.shape[0] != n or t.shape[2] != d:
-            _refuse("rows or head_dim of %s differ" % name)
-    if (q_out is not None and (q is None or q_out.shape != q.shape)) or (k_out is not None and (k is None or k_out.shape != k.shape)):
-        _refuse("an output's shape differs from its input's")
-    desc = RopeRowsDesc(_DTYPES[ref.dtype], n, 0 if q is None else q.shape[1], 0 if k is None else k.shape[1], d,
-                        2 * freq.numel(), layout, magnitude, *strides)
-    _launch(ref.device, stream, lib.keep_rope_rows, C.byref(desc), _ptr(q), _ptr(q_out), _ptr(k), _ptr(k_out),
-            _array("positions", positions, torch.int32, n, ref.device),
-            _array("freq", freq, torch.float64, freq.numel(), ref.device))
+    device, dtype = ref.device, ref.dtype
+    if dtype not in _DTYPES or ref.dim() != 3 or (q is None and q_out is not None) or (k is None and k_out is not None):
+        _refuse("queries and keys must be [rows, heads, head_dim] in float32 or bfloat16, outputs go with inputs")
+    n, _, d = ref.shape
+    hq = hkv = qi = qo = ki = ko = 0
+    if q is not None:
+        q_out = q if q_out is None else q_out
+        hq, qi, qo = q.shape[1], _heads("q", q, device, dtype), _heads("q_out", q_out, device, dtype)
+        if q_out.shape != q.shape:
+            _refuse("the shape of q_out differs from that of q")
+    if k is not None:
+        k_out = k if k_out is None else k_out
+        ki, ko = _heads("k", k, device, dtype), _heads("k_out", k_out, device, dtype)
+        rows, hkv, dk = k.shape
+        if k_out.shape != k.shape or rows != n or dk != d:
+            _refuse("rows or head_dim of keys differ from the queries', or k_out from k")
+    pairs = freq.numel()
+    desc = RopeRowsDesc(_DTYPES[dtype], n, hq, hkv, d, 2 * pairs, layout, magnitude, qi, qo, ki, ko)
+    _launch(device, stream, lib.keep_rope_rows, C.byref(desc), _ptr(q), _ptr(q_out), _ptr(k), _ptr(k_out),
+            _array("positions", positions, torch.int32, n, device), _array("freq", freq, torch.float64, pairs, device))
     return q_out, k_out
 
 
@@ -439,11 +448,11 @@ class PagedCache:
 
     def _rows(self, call, k, v, slots, stream):
         stride = _heads("k", k, self.device)
-        if _heads("v", v, self.device, k.dtype) != stride or v.shape != k.shape or \
-                tuple(k.shape[1:]) != (self.c.n_kv_heads, self.c.head_dim):
+        n, h, d = k.shape
+        if _heads("v", v, self.device, k.dtype) != stride or v.shape != k.shape or h != self.c.n_kv_heads or d != self.c.head_dim:
             _refuse("k and v must be alike, [rows, n_kv_heads, head_dim]")
-        _launch(self.device, stream, call, C.byref(self.c), _DTYPES[k.dtype], k.data_ptr(), v.data_ptr(), k.shape[0], stride,
-                _array("slots", slots, torch.int32, k.shape[0], self.device))
+        _launch(self.device, stream, call, C.byref(self.c), _DTYPES[k.dtype], k.data_ptr(), v.data_ptr(), n, stride,
+                _array("slots", slots, torch.int32, n, self.device))
 
     def write(self, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, stream=None):
         """keep_cache_write: rows k, v [n, n_kv_heads, head_dim] into the slots (int32 [n])"""

@@ -11,7 +11,7 @@
 // Sums are of whole numbers, so neither atomics nor the division among threads can change a result.  A row is read three times
 // (HBM the first time).  A list that does not fit (thousands of equal or nearly equal logits in a bin) is left to find_token,
 // which divides the bin further by the bits of the logits.  Few rows are divided among workgroups, a launch per step, with the
-// histogram and the list in the workspace; from 129 rows on a workgroup does a whole row in LDS.
+// histogram and the list in the workspace; else a workgroup does a whole row in LDS.
 #include <algorithm>
 
 #include "serve_common.h"
@@ -25,7 +25,11 @@ constexpr double T_MAX = 41.25;       // beyond t = 41 a weight rounds to zero
 constexpr double T_SCALE = BINS / T_MAX;
 constexpr double ONE = 1099511627776.0;  // 2^40
 constexpr int LIST = 2048;            // tokens that are ranked among themselves
-constexpr int WIDE_ROWS = 128, MAX_PARTS = 16;
+constexpr int MAX_PARTS = 16;
+// Rows are divided up to 64 of them, and from 40 000 tokens on: a launch per step costs some 15 us more than one kernel.  us divided /
+// whole: 64 rows of 16 000 29 / 17, 32 000 30 / 20 (weighing all 43 / 37), 64 000 30 / 27, 152 064 weighing all 67 / 110;
+// 128 rows of 152 064 57 / 49.
+constexpr int WIDE_ROWS = 64, WIDE_VOCAB = 40000;
 
 // Larger numbers first, NaN last; -0 equals +0
 __device__ __forceinline__ uint32_t order_key(float v) {
@@ -795,10 +799,13 @@ __global__ void __launch_bounds__(CT) k_sample_choose(SampleArgs a) {
 
 // Bytes of the workspace's pieces for one row
 constexpr int64_t ROW_BYTES = MAX_PARTS * 8 + BINS * 12 + LIST * 8 + sizeof(Plan) + 4;
-uint64_t workspace_bytes(int32_t n_rows) { return n_rows <= WIDE_ROWS ? 256 + n_rows * ((ROW_BYTES + 255) / 256 * 256) : 256; }
+bool is_wide(int32_t n_rows, int32_t vocab) { return n_rows <= WIDE_ROWS && vocab >= WIDE_VOCAB; }
+uint64_t workspace_bytes(int32_t n_rows, int32_t vocab) {
+  return is_wide(n_rows, vocab) ? 256 + n_rows * ((ROW_BYTES + 255) / 256 * 256) : 256;
+}
 
 void launch(SampleArgs a, void* workspace, hipStream_t s) {
-  if (a.n_rows > WIDE_ROWS) {
+  if (!is_wide(a.n_rows, a.vocab)) {
     hipLaunchKernelGGL(k_sample_row, dim3(a.n_rows), dim3(ST), 0, s, a);
     return;
   }
@@ -827,7 +834,7 @@ void launch(SampleArgs a, void* workspace, hipStream_t s) {
 
 }  // namespace
 
-uint64_t sample_decode_bytes() { return workspace_bytes(1); }
+uint64_t sample_decode_bytes() { return workspace_bytes(1, KEEP_SAMPLE_MAX_VOCAB); }
 
 void launch_sample_decode(const float* logits, int32_t vocab, const float* d_uniform, const keep_sampling& how, int32_t* token,
                           float* prob, void* workspace, hipStream_t s) {
@@ -854,7 +861,7 @@ using namespace keep;
 
 extern "C" uint64_t keep_sample_workspace_bytes(int32_t n_rows, int32_t vocab) {
   if (n_rows < 0 || n_rows > 65535 || vocab < 1 || vocab > KEEP_SAMPLE_MAX_VOCAB) return 0;
-  return workspace_bytes(n_rows);
+  return workspace_bytes(n_rows, vocab);
 }
 
 extern "C" keep_status keep_sample(const keep_sample_desc* d, const void* logits, const float* uniform,
