@@ -265,7 +265,7 @@ __device__ __forceinline__ void paged_finish(const PagedArgs& a, const PagedPlac
                                 p.head};
 }
 
-void launch_paged_generic(const PagedArgs& a, hipStream_t s);
+void launch_paged_generic(const PagedArgs& a, int rows, hipStream_t s);  // tiles of 16 or 32 query rows
 // bf16 queries, heads of 64 or 128, a bf16 or 8-bit cache of less than 64 GB per tensor; rows: query rows of a tile (16, 32 or 128)
 void launch_paged_mfma(const PagedArgs& a, int rows, hipStream_t s);
 void launch_paged_join(const PagedArgs& a, int rows, hipStream_t s);

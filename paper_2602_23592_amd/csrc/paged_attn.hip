@@ -12,27 +12,31 @@ namespace {
 
 using f32x4 = paged_f32x4;
 
-constexpr int GT_ROWS = 16, GT_KEYS = 64;
+constexpr int GT_KEYS = 64;
 
-__device__ __forceinline__ float load_value(const void* p, int64_t i, int dtype) {
-  return dtype == KEEP_F32 ? static_cast<const float*>(p)[i] : bf16_bits_to_f32(static_cast<const uint16_t*>(p)[i]);
-}
-
-// Four values of a cache from element i on, as the numbers they stand for
-__device__ __forceinline__ f32x4 load_cached(const void* p, int64_t i, int format, float scale) {
-  if (format == KEEP_CACHE_F32) return *reinterpret_cast<const f32x4*>(static_cast<const float*>(p) + i);
-  if (format == KEEP_CACHE_BF16) {
+// Four values as they lie in memory, from element i on, and the numbers they stand for
+template <int FORMAT>
+__device__ __forceinline__ uint4 load_raw(const void* p, int64_t i) {
+  if (FORMAT == KEEP_CACHE_F32) return *reinterpret_cast<const uint4*>(static_cast<const float*>(p) + i);
+  if (FORMAT == KEEP_CACHE_BF16) {
     const uint2 u = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + i);
-    return f32x4{bf16_bits_to_f32((uint16_t)u.x), bf16_bits_to_f32((uint16_t)(u.x >> 16)),
-                 bf16_bits_to_f32((uint16_t)u.y), bf16_bits_to_f32((uint16_t)(u.y >> 16))};
+    return make_uint4(u.x, u.y, 0, 0);
   }
-  const uint32_t u = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(p) + i);
-  if (format == KEEP_CACHE_FP8) {
-    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)u, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)u, true);
+  return make_uint4(*reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(p) + i), 0, 0, 0);
+}
+template <int FORMAT>
+__device__ __forceinline__ f32x4 value_of(uint4 u, float scale) {
+  if (FORMAT == KEEP_CACHE_F32)
+    return f32x4{__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)};
+  if (FORMAT == KEEP_CACHE_BF16)
+    return f32x4{__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
+                 __uint_as_float(u.y & 0xffff0000u)};
+  if (FORMAT == KEEP_CACHE_FP8) {
+    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)u.x, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)u.x, true);
     return f32x4{lo[0] * scale, lo[1] * scale, hi[0] * scale, hi[1] * scale};
   }
-  return f32x4{(float)(int8_t)u * scale, (float)(int8_t)(u >> 8) * scale, (float)(int8_t)(u >> 16) * scale,
-               (float)(int8_t)(u >> 24) * scale};
+  return f32x4{(float)(int8_t)u.x * scale, (float)(int8_t)(u.x >> 8) * scale, (float)(int8_t)(u.x >> 16) * scale,
+               (float)(int8_t)(u.x >> 24) * scale};
 }
 
 __device__ __forceinline__ bool finite4(f32x4 v) {
@@ -42,138 +46,200 @@ __device__ __forceinline__ bool finite4(f32x4 v) {
   return ok;
 }
 
-// Any types, head_dim a multiple of 16 up to 16 * ND.  A worker's tile is 16 query rows and 64 keys; each of the four waves takes
-// 16 of the keys for all rows, with statistics and output of its own, added at a job's end.  S^T = K . Q^T leaves a lane one
-// query row (lane % 16) and four keys (4 (lane / 16) + r), which is the operand that O^T = V^T . P^T wants from it in step r:
-// the probabilities never leave their registers.  Rows of K and V in LDS are padded by four values, so that both operand
-// reads meet all banks.
+// A thread's share of a key tile: every fourth four values of one key
 template <int ND>
-__global__ void __launch_bounds__(256) k_paged_generic(PagedArgs a) {
+struct GenericShare {
+  int64_t at, scale_at;  // -1: behind the sequence's end
+  uint4 raw[ND];
+  float scale;
+};
+template <int ND>
+__device__ __forceinline__ void generic_locate(const PagedArgs& a, const PagedPlace& p, const PagedSeq& q, const int32_t* table,
+                                               int kt, GenericShare<ND>& f) {
+  const int key = kt * GT_KEYS + (threadIdx.x >> 2);
+  f.at = -1;
+  if (key >= q.len) return;
+  f.at = paged_key(a, table, key, f.scale_at) + p.head * a.c.head_stride + (threadIdx.x & 3) * 4;
+  f.scale_at += (int64_t)p.head * a.c.page_size;
+}
+template <int FORMAT, int ND>
+__device__ __forceinline__ void generic_load(const PagedArgs& a, const void* values, const float* scales, GenericShare<ND>& f) {
+  f.scale = 1.f;
+#pragma unroll
+  for (int j = 0; j < ND; ++j) f.raw[j] = make_uint4(0, 0, 0, 0);
+  if (f.at < 0) return;
+  if (FORMAT == KEEP_CACHE_FP8 || FORMAT == KEEP_CACHE_INT8) f.scale = scales[f.scale_at];
+#pragma unroll
+  for (int j = 0; j < ND; ++j)
+    if (16 * j < a.c.head_dim) f.raw[j] = load_raw<FORMAT>(values, f.at + 16 * j);
+}
+// ... to LDS; returns whether all are finite
+template <int FORMAT, int ND>
+__device__ __forceinline__ bool generic_store(float* tile, const GenericShare<ND>& f) {
+  float* to = tile + (threadIdx.x >> 2) * (16 * ND + 4) + (threadIdx.x & 3) * 4;
+  bool ok = true;
+#pragma unroll
+  for (int j = 0; j < ND; ++j) {
+    const f32x4 v = value_of<FORMAT>(f.raw[j], f.scale);
+    ok = ok && finite4(v);
+    *reinterpret_cast<f32x4*>(to + 16 * j) = v;
+  }
+  return ok;
+}
+
+// Any types, head_dim a multiple of 16 up to 16 * ND.  A worker's tile is 16 RB query rows and 64 keys; each of the four waves takes
+// 16 of the keys for all rows, with statistics and output of its own, added at a job's end.  S^T = K . Q^T leaves a lane one
+// query row (lane % 16) of each 16 and four keys (4 (lane / 16) + r), which is the operand that O^T = V^T . P^T wants from it in
+// step r: the probabilities never leave their registers.  Rows of K and V in LDS are padded by four values, so that both operand
+// reads meet all banks.  V is on its way to registers while the scores are formed, the next tile's K during the second product.
+template <int FORMAT, int ND, int RB>
+__global__ void __launch_bounds__(256, ND <= 8 ? 2 : 1) k_paged_generic(PagedArgs a) {
+  constexpr int TR = 16 * RB;
   extern __shared__ __attribute__((aligned(16))) float lds[];
-  __shared__ int odd;  // some value of the tile is not finite
+  __shared__ int odd[2];  // some value of the tile (by turns) is not finite
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, g = lane >> 4;
-  const int dh = a.c.head_dim, nd = dh / 16, stride = dh + 4;
+  const int dh = a.c.head_dim, nd = dh / 16;
+  constexpr int stride = 16 * ND + 4;
   const int worker = blockIdx.x;
   PagedSeq q;
-  PagedPlace p = paged_place<GT_ROWS, GT_KEYS>(a, worker, reinterpret_cast<uint64_t*>(lds), q);
+  PagedPlace p = paged_place<TR, GT_KEYS>(a, worker, reinterpret_cast<uint64_t*>(lds), q);
   if (tid == 0) a.rec[worker].last = 0;
   if (p.begin >= p.end) return;
   float* sk = lds;
   float* sv = lds + GT_KEYS * stride;
-  float* sml = sv + GT_KEYS * stride;  // [2][4 waves][16]
+  float* sml = sv + GT_KEYS * stride;  // [2][4 waves][TR]
   for (uint64_t at = p.begin;;) {
-    const PagedPart part = paged_part<GT_ROWS, GT_KEYS>(a, p, q, at);
+    const PagedPart part = paged_part<TR, GT_KEYS>(a, p, q, at);
     if (part.u0 == part.u1) break;  // (the run's last step)
-    const int x = p.tile * GT_ROWS + col;
-    const bool valid = x < q.rows * a.rep;
-    const int token = valid ? (int)div_by(x, a.by_rep) : 0;
-    const int head = p.head * a.rep + (valid ? x - token * a.rep : 0);
-    const int pos = valid ? q.len - q.rows + token : -1;
-    const int lo = a.window ? max(0, pos - a.window + 1) : 0;
-    float qf[4 * ND];
-    const int64_t q_at = (int64_t)(q.row0 + token) * a.q_stride + (int64_t)head * dh + g * (dh / 4);
-#pragma unroll
-    for (int i = 0; i < 4 * ND; ++i) qf[i] = i < 4 * nd ? load_value(a.q, q_at + i, a.dtype) : 0.f;
-    f32x4 acc[ND];
-#pragma unroll
-    for (int i = 0; i < ND; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, l = 0.f;
     const int32_t* table = a.table + (int64_t)p.seq * a.max_pages;
-
-    for (int kt = part.first + part.u0; kt < part.first + part.u1; ++kt) {
-      __syncthreads();  // the tile before has been read
-      if (tid == 0) odd = 0;
-      __syncthreads();
-      bool ok = true;
-      for (int i = tid; i < GT_KEYS * (dh / 4); i += 256) {
-        const int row = i / (dh / 4), d = (i - row * (dh / 4)) * 4, key = kt * GT_KEYS + row;
-        f32x4 k{0.f, 0.f, 0.f, 0.f}, v = k;
-        if (key < q.len) {
-          int64_t sc;
-          const int64_t e = paged_key(a, table, key, sc) + p.head * a.c.head_stride + d;
-          sc += (int64_t)p.head * a.c.page_size;
-          const bool scaled = a.c.k_scale != nullptr;
-          k = load_cached(a.c.k, e, a.c.format, scaled ? a.c.k_scale[sc] : 1.f);
-          v = load_cached(a.c.v, e, a.c.format, scaled ? a.c.v_scale[sc] : 1.f);
-        }
-        ok = ok && finite4(v);
-        *reinterpret_cast<f32x4*>(sk + row * stride + d) = k;
-        *reinterpret_cast<f32x4*>(sv + row * stride + d) = v;
+    const int kt1 = part.first + part.u1;
+    GenericShare<ND> next;
+    generic_locate(a, p, q, table, part.first + part.u0, next);
+    generic_load<FORMAT>(a, a.c.k, a.c.k_scale, next);
+    int pos[RB], lo[RB];
+    f32x4 qf[RB][ND], acc[RB][ND];
+    float m[RB], l[RB];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+      const int x = p.tile * TR + 16 * b + col;
+      const bool valid = x < q.rows * a.rep;
+      const int token = valid ? (int)div_by(x, a.by_rep) : 0;
+      const int head = p.head * a.rep + (valid ? x - token * a.rep : 0);
+      pos[b] = valid ? q.len - q.rows + token : -1;
+      lo[b] = a.window ? max(0, pos[b] - a.window + 1) : 0;
+      const int64_t q_at = (int64_t)(q.row0 + token) * a.q_stride + (int64_t)head * dh + g * 4 * ND;
+#pragma unroll
+      for (int i = 0; i < ND; ++i) qf[b][i] = acc[b][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (a.dtype == KEEP_F32) {
+#pragma unroll
+        for (int i = 0; i < ND; ++i)
+          if (g * 4 * ND + 4 * i < dh) qf[b][i] = value_of<KEEP_CACHE_F32>(load_raw<KEEP_CACHE_F32>(a.q, q_at + 4 * i), 1.f);
+      } else {
+#pragma unroll
+        for (int i = 0; i < ND; ++i)
+          if (g * 4 * ND + 4 * i < dh) qf[b][i] = value_of<KEEP_CACHE_BF16>(load_raw<KEEP_CACHE_BF16>(a.q, q_at + 4 * i), 1.f);
       }
-      if (!ok) odd = 1;
+      m[b] = -INFINITY;
+      l[b] = 0.f;
+    }
+    __syncthreads();  // the LDS of the division, or of the job before, has been read
+    if (tid == 0) odd[0] = odd[1] = 0;
+    for (int kt = part.first + part.u0; kt < kt1; ++kt) {
+      const int turn = (kt - part.first - part.u0) & 1;
+      generic_store<FORMAT>(sk, next);
       __syncthreads();
-      const float* wk = sk + (wave * 16 + col) * stride + g * (dh / 4);
-      f32x4 s{0.f, 0.f, 0.f, 0.f};
+      generic_load<FORMAT>(a, a.c.v, a.c.v_scale, next);
+      const float* wk = sk + (wave * 16 + col) * stride + g * 4 * ND;
+      f32x4 s[RB];
+#pragma unroll
+      for (int b = 0; b < RB; ++b) s[b] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < ND; ++i) {
-        if (i >= nd) continue;
         const f32x4 k = *reinterpret_cast<const f32x4*>(wk + 4 * i);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k[e], qf[4 * i + e], s, 0, 0, 0);
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int b = 0; b < RB; ++b) s[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[e], qf[b][i][e], s[b], 0, 0, 0);
       }
       const int key0 = kt * GT_KEYS + wave * 16;
-      float top = -INFINITY;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int key = key0 + 4 * g + r;
-        s[r] = key <= pos && key >= lo ? s[r] * a.scale_log2e : -INFINITY;
-        top = fmaxf(top, s[r]);
+      for (int b = 0; b < RB; ++b) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int key = key0 + 4 * g + r;
+          s[b][r] = key <= pos[b] && key >= lo[b] ? s[b][r] * a.scale_log2e : -INFINITY;
+          top = fmaxf(top, s[b][r]);
+        }
+        top = fmaxf(top, __shfl_xor(top, 16, 64));
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const float m_new = fmaxf(m[b], top), m_ref = m_new == -INFINITY ? 0.f : m_new;
+        if (__ballot(m_new != m[b])) {
+          const float alpha = __builtin_amdgcn_exp2f(m[b] - m_ref);
+          l[b] *= alpha;
+#pragma unroll
+          for (int i = 0; i < ND; ++i) acc[b][i] *= alpha;
+          m[b] = m_new;
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          s[b][r] = __builtin_amdgcn_exp2f(s[b][r] - m_ref);
+          l[b] += s[b][r];
+        }
       }
-      top = fmaxf(top, __shfl_xor(top, 16, 64));
-      top = fmaxf(top, __shfl_xor(top, 32, 64));
-      const float m_new = fmaxf(m, top), m_ref = m_new == -INFINITY ? 0.f : m_new;
-      if (__ballot(m_new != m)) {
-        const float alpha = __builtin_amdgcn_exp2f(m - m_ref);
-        l *= alpha;
-#pragma unroll
-        for (int i = 0; i < ND; ++i) acc[i] *= alpha;
-        m = m_new;
-      }
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        s[r] = __builtin_amdgcn_exp2f(s[r] - m_ref);
-        l += s[r];
+      if (!generic_store<FORMAT>(sv, next)) odd[turn] = 1;
+      __syncthreads();
+      if (tid == 0) odd[turn ^ 1] = 0;
+      if (kt + 1 < kt1) {
+        generic_locate(a, p, q, table, kt + 1, next);
+        generic_load<FORMAT>(a, a.c.k, a.c.k_scale, next);
       }
       const float* wv = sv + (wave * 16) * stride;
-      if (!odd) {
+      if (!odd[turn]) {
 #pragma unroll
-        for (int i = 0; i < ND; ++i) {
-          if (i >= nd) continue;
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            acc[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(wv[(4 * g + r) * stride + 16 * i + col], s[r], acc[i], 0, 0, 0);
-        }
-      } else {
-        // a product with a probability of zero would carry infinities and NaN to rows that do not see the key
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const float pj = __shfl(s[j & 3], (j >> 2) * 16 + col, 64);
-          const bool sees = key0 + j <= pos && key0 + j >= lo;
+        for (int r = 0; r < 4; ++r)
 #pragma unroll
           for (int i = 0; i < ND; ++i) {
-            if (i >= nd) continue;
-            const f32x4 v = *reinterpret_cast<const f32x4*>(wv + j * stride + 16 * i + 4 * g);
+            const float v = wv[(4 * g + r) * stride + 16 * i + col];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) acc[i][r] += sees ? pj * v[r] : 0.f;
+            for (int b = 0; b < RB; ++b) acc[b][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, s[b][r], acc[b][i], 0, 0, 0);
+          }
+      } else {
+        // a product with a probability of zero would carry infinities and NaN to rows that do not see the key
+#pragma unroll 1
+        for (int j = 0; j < 16; ++j) {
+#pragma unroll
+          for (int b = 0; b < RB; ++b) {
+            const float pj = __shfl(j & 2 ? j & 1 ? s[b][3] : s[b][2] : j & 1 ? s[b][1] : s[b][0], (j >> 2) * 16 + col, 64);
+            const bool sees = key0 + j <= pos[b] && key0 + j >= lo[b];
+#pragma unroll
+            for (int i = 0; i < ND; ++i) {
+              const f32x4 v = *reinterpret_cast<const f32x4*>(wv + j * stride + 16 * i + 4 * g);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) acc[b][i][e] += sees ? pj * v[e] : 0.f;
+            }
           }
         }
       }
     }
 
     // ---- the four waves' parts, in their order
-    l += __shfl_xor(l, 16, 64);
-    l += __shfl_xor(l, 32, 64);
     __syncthreads();
-    if (g == 0) sml[wave * 16 + col] = m, sml[64 + wave * 16 + col] = l;
-    float* so = lds;  // [4 waves][dh / 4][16][4]
+    float* so = lds;  // [4 waves][dh / 4][TR][4]
 #pragma unroll
-    for (int i = 0; i < ND; ++i)
-      if (i < nd) *reinterpret_cast<f32x4*>(so + ((wave * (dh / 4) + 4 * i + g) * 16 + col) * 4) = acc[i];
+    for (int b = 0; b < RB; ++b) {
+      l[b] += __shfl_xor(l[b], 16, 64);
+      l[b] += __shfl_xor(l[b], 32, 64);
+      if (g == 0) sml[wave * TR + 16 * b + col] = m[b], sml[(4 + wave) * TR + 16 * b + col] = l[b];
+#pragma unroll
+      for (int i = 0; i < ND; ++i)
+        if (i < nd) *reinterpret_cast<f32x4*>(so + ((wave * (dh / 4) + 4 * i + g) * TR + 16 * b + col) * 4) = acc[b][i];
+    }
     __syncthreads();
-    paged_finish<GT_ROWS>(a, p, q, part, worker, so, sml);
+    paged_finish<TR>(a, p, q, part, worker, so, sml);
     at += part.steps;
     if (at >= p.end) break;
-    paged_next<GT_ROWS>(a, p, q);
+    paged_next<TR>(a, p, q);
   }
 }
 
@@ -300,15 +366,32 @@ constexpr uint64_t REC_BYTES = (PAGED_WORKERS * sizeof(PagedRecord) + 255) & ~(u
 
 }  // namespace
 
-void launch_paged_generic(const PagedArgs& a, hipStream_t s) {
-  const int dh = a.c.head_dim;
+template <int FORMAT, int ND, int RB>
+static void launch_generic(const PagedArgs& a, hipStream_t s) {
   // tiles (or the waves' outputs, which need no more) and statistics; the division of the work before that
-  const size_t lds = std::max<size_t>(((size_t)2 * GT_KEYS * (dh + 4) + 128) * sizeof(float), (size_t)8 * (a.n_seqs + 260));
-  const auto kernel = dh <= 64 ? k_paged_generic<4> : dh <= 128 ? k_paged_generic<8> : k_paged_generic<16>;
-  static std::atomic<uint64_t> done[3];
-  set_max_dyn_smem_once(done[dh <= 64 ? 0 : dh <= 128 ? 1 : 2], reinterpret_cast<const void*>(kernel), 150 * 1024);
-  hipLaunchKernelGGL(kernel, dim3(PAGED_WORKERS), dim3(256), lds, s, a);
-  launch_paged_join(a, GT_ROWS, s);
+  const size_t lds = std::max<size_t>(((size_t)2 * GT_KEYS * (16 * ND + 4) + 8 * 16 * RB) * sizeof(float), (size_t)8 * (a.n_seqs + 260));
+  static std::atomic<uint64_t> done{0};
+  set_max_dyn_smem_once(done, reinterpret_cast<const void*>(k_paged_generic<FORMAT, ND, RB>), 150 * 1024);
+  hipLaunchKernelGGL((k_paged_generic<FORMAT, ND, RB>), dim3(PAGED_WORKERS), dim3(256), lds, s, a);
+  launch_paged_join(a, 16 * RB, s);
+}
+template <int FORMAT>
+static void launch_generic(const PagedArgs& a, int rows, hipStream_t s) {
+  const int dh = a.c.head_dim;
+  if (rows == 16)
+    dh <= 64 ? launch_generic<FORMAT, 4, 1>(a, s) : dh <= 80 ? launch_generic<FORMAT, 5, 1>(a, s)
+    : dh <= 128 ? launch_generic<FORMAT, 8, 1>(a, s) : launch_generic<FORMAT, 16, 1>(a, s);
+  else
+    dh <= 64 ? launch_generic<FORMAT, 4, 2>(a, s) : dh <= 80 ? launch_generic<FORMAT, 5, 2>(a, s) : launch_generic<FORMAT, 8, 2>(a, s);
+}
+
+void launch_paged_generic(const PagedArgs& a, int rows, hipStream_t s) {
+  switch (a.c.format) {
+    case KEEP_CACHE_F32: return launch_generic<KEEP_CACHE_F32>(a, rows, s);
+    case KEEP_CACHE_BF16: return launch_generic<KEEP_CACHE_BF16>(a, rows, s);
+    case KEEP_CACHE_FP8: return launch_generic<KEEP_CACHE_FP8>(a, rows, s);
+    default: return launch_generic<KEEP_CACHE_INT8>(a, rows, s);
+  }
 }
 
 void launch_paged_join(const PagedArgs& a, int rows, hipStream_t s) {
@@ -327,7 +410,7 @@ using namespace keep;
 extern "C" uint64_t keep_paged_attention_workspace_bytes(const keep_paged_cache* cache, int32_t n_q_heads, int32_t n_seqs) {
   if (check_cache(cache, "keep_paged_attention_workspace_bytes") != KEEP_OK) return 0;
   if (n_q_heads < 1 || n_q_heads % cache->n_kv_heads || n_seqs < 0 || n_seqs > KEEP_PAGED_MAX_SEQS) return 0;
-  return REC_BYTES + part_bytes(has_mfma(cache) ? 128 : GT_ROWS, cache->head_dim);
+  return REC_BYTES + part_bytes(has_mfma(cache) ? 128 : 32, cache->head_dim);
 }
 
 extern "C" keep_status keep_paged_attention(const keep_paged_attention_desc* d, const keep_paged_cache* cache, const void* q,
@@ -395,11 +478,11 @@ extern "C" keep_status keep_paged_attention(const keep_paged_attention_desc* d, 
   // 59 / 56 / 64, 89 / 67 / 75.  Up to 16 rows a tile of 32 has nothing to gain.
   const bool mfma = d->dtype == KEEP_BF16 && has_mfma(cache);
   const int64_t mean = (d->n_rows * (int64_t)a.rep + d->n_seqs - 1) / d->n_seqs;
-  const int rows = !mfma || mean <= 16 ? 16 : mean <= 48 ? 32 : 128;
+  const int rows = mean <= 16 || cache->head_dim > 128 ? 16 : !mfma || mean <= 48 ? 32 : 128;
   a.part_o = a.part_ml + (size_t)2 * PAGED_WORKERS * 2 * rows;
   if (mfma)
     launch_paged_mfma(a, rows, static_cast<hipStream_t>(stream));
   else
-    launch_paged_generic(a, static_cast<hipStream_t>(stream));
+    launch_paged_generic(a, rows, static_cast<hipStream_t>(stream));
   return launched(me);
 }
