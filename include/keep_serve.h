@@ -145,8 +145,8 @@ uint64_t keep_paged_attention_workspace_bytes(const keep_paged_cache* cache, int
  *   workspace: DEVICE, 256-byte aligned, at least keep_paged_attention_workspace_bytes.
  * Rows of out and lse that no sequence owns are left as they were.  A key or value that is not finite reaches only the
  * rows that see it.  Sums and statistics are binary32 in an order that depends on the lengths alone, so equal calls give
- * equal bits.  bf16 queries with heads of 64 or 128 over a bf16 or 8-bit cache run on the bf16 matrix instruction, with the probabilities
- * rounded to bf16; everything else on the fp32 one.
+ * equal bits.  bf16 queries with heads of 64, 128 or 256 over a bf16 or 8-bit cache run on the bf16 matrix instruction,
+ * with the probabilities rounded to bf16; everything else on the fp32 one.
  * Errors: INVALID_ARG, SHAPE, WORKSPACE (workspace_bytes too small), HIP. */
 keep_status keep_paged_attention(const keep_paged_attention_desc* desc, const keep_paged_cache* cache, const void* q,
                                  const int32_t* q_start, const int32_t* kv_len, const int32_t* page_table, void* out,

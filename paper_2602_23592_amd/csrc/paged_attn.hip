@@ -359,7 +359,7 @@ uint64_t part_bytes(int tr, int dh) { return (uint64_t)2 * PAGED_WORKERS * tr * 
 bool has_mfma(const keep_paged_cache* c) {
   const int64_t span = (int64_t)(c->n_pages - 1) * c->page_stride + (int64_t)(c->n_kv_heads - 1) * c->head_stride +
                        (int64_t)(c->page_size - 1) * c->token_stride + c->head_dim;
-  return c->format != KEEP_CACHE_F32 && (c->head_dim == 64 || c->head_dim == 128) &&
+  return c->format != KEEP_CACHE_F32 && (c->head_dim == 64 || c->head_dim == 128 || c->head_dim == 256) &&
          span * format_size(c->format) < (int64_t)64 << 30;
 }
 constexpr uint64_t REC_BYTES = (PAGED_WORKERS * sizeof(PagedRecord) + 255) & ~(uint64_t)255;
@@ -410,7 +410,7 @@ using namespace keep;
 extern "C" uint64_t keep_paged_attention_workspace_bytes(const keep_paged_cache* cache, int32_t n_q_heads, int32_t n_seqs) {
   if (check_cache(cache, "keep_paged_attention_workspace_bytes") != KEEP_OK) return 0;
   if (n_q_heads < 1 || n_q_heads % cache->n_kv_heads || n_seqs < 0 || n_seqs > KEEP_PAGED_MAX_SEQS) return 0;
-  return REC_BYTES + part_bytes(has_mfma(cache) ? 128 : 32, cache->head_dim);
+  return REC_BYTES + part_bytes(has_mfma(cache) && cache->head_dim <= 128 ? 128 : 32, cache->head_dim);
 }
 
 extern "C" keep_status keep_paged_attention(const keep_paged_attention_desc* d, const keep_paged_cache* cache, const void* q,
@@ -478,7 +478,7 @@ extern "C" keep_status keep_paged_attention(const keep_paged_attention_desc* d, 
   // 59 / 56 / 64, 89 / 67 / 75.  Up to 16 rows a tile of 32 has nothing to gain.
   const bool mfma = d->dtype == KEEP_BF16 && has_mfma(cache);
   const int64_t mean = (d->n_rows * (int64_t)a.rep + d->n_seqs - 1) / d->n_seqs;
-  const int rows = mean <= 16 || cache->head_dim > 128 ? 16 : !mfma || mean <= 48 ? 32 : 128;
+  const int rows = mean <= 16 || (!mfma && cache->head_dim > 128) ? 16 : !mfma || mean <= 48 || cache->head_dim > 128 ? 32 : 128;
   a.part_o = a.part_ml + (size_t)2 * PAGED_WORKERS * 2 * rows;
   if (mfma)
     launch_paged_mfma(a, rows, static_cast<hipStream_t>(stream));

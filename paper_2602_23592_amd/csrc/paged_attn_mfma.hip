@@ -1,4 +1,4 @@
-// Attention over pages on the bf16 matrix instruction: bf16 queries, heads of 64 or 128, a bf16 or 8-bit cache.
+// Attention over pages on the bf16 matrix instruction: bf16 queries, heads of 64, 128 or 256, a bf16 or 8-bit cache.
 //
 // k_paged_few: tiles of 16 or 32 query rows (one to a few tokens with their heads), where the keys are read once for few rows and
 // memory is the bound.  Each of a workgroup's four waves streams key slices of its own (32 of a unit's 128 keys) through its own
@@ -89,11 +89,12 @@ __device__ __forceinline__ bf16x8 codes8(uint32_t lo, uint32_t hi) {
 // CH: chunks per row; 16 / CH rows share a stretch of 256 bytes, the chunks of those that lie at the same place move apart.
 template <int CH>
 __device__ __forceinline__ int k_chunk(int row, int c) {
-  return CH == 16 ? c ^ (row & 15) : CH == 8 ? c ^ ((row >> 1) & 7) : c ^ ((row >> 2) & 3);
+  return CH >= 16 ? c ^ (row & 15) : CH == 8 ? c ^ ((row >> 1) & 7) : c ^ ((row >> 2) & 3);
 }
 template <int CH, bool WIDE>  // WIDE: bf16
 __device__ __forceinline__ int v_chunk(int row, int c) {
-  if (WIDE) return CH == 16 ? c ^ (2 * (row & 7)) : c ^ (2 * ((row >> 1) & 3));
+  if (WIDE) return CH >= 16 ? c ^ (2 * (row & 7)) : c ^ (2 * ((row >> 1) & 3));
+  if (CH == 16) return c ^ ((row & 7) | ((row >> 1) & 8));
   return CH == 8 ? c ^ (((row >> 1) & 3) | ((row >> 2) & 4)) : c ^ (((row >> 2) & 1) | ((row >> 3) & 2));
 }
 
@@ -107,7 +108,8 @@ struct Few {
   static constexpr int ROW = DH * (WIDE ? 2 : 1), CH = ROW / 16;  // bytes and chunks of a key
   static constexpr int PER = 64 / CH, NI = SLICE / PER;           // rows of a load, loads of a slice
   static constexpr int BYTES = SLICE * ROW;
-  static constexpr int NS = 16384 / (2 * BYTES);                  // slices in flight
+  static constexpr int HELD = TR * DH * 4 > 16384 ? TR * DH * 4 : 16384;            // bytes of a wave: its slices, at the end its output
+  static constexpr int NS = 2 * BYTES < HELD ? HELD / (2 * BYTES) : 1;              // slices in flight
   static constexpr int NK = NI + (WIDE ? 0 : 1), NV = NI;         // loads of a slice's K (with the scales) and V
   static constexpr int WAVE = NS * (2 * BYTES + (WIDE ? 0 : 256));
   static constexpr int ML = 4 * WAVE, TBL = ML + 8 * TR * 4, LDS = TBL + TABLE * 4;
@@ -115,7 +117,7 @@ struct Few {
 };
 
 template <int DH, int FMT, int RB>
-__global__ void __launch_bounds__(256, 2) k_paged_few(PagedArgs a) {
+__global__ void __launch_bounds__(256, (Few<DH, FMT, RB>::LDS > 80 * 1024 ? 1 : 2)) k_paged_few(PagedArgs a) {
   using F = Few<DH, FMT, RB>;
   constexpr int TR = F::TR, ROW = F::ROW, CH = F::CH, NS = F::NS, DT = DH / 16, KS = DH / 32;
   extern __shared__ __attribute__((aligned(256))) char lds[];
@@ -237,9 +239,9 @@ __global__ void __launch_bounds__(256, 2) k_paged_few(PagedArgs a) {
         // K of this slice has landed; behind it V and `left` whole slices were requested
         switch (left) {
           case 0: vm_wait<F::NV>(); break;
-          case 1: vm_wait<F::NV + F::NK + F::NV>(); break;
-          case 2: vm_wait<F::NV + 2 * (F::NK + F::NV)>(); break;
-          default: vm_wait<F::NV + 3 * (F::NK + F::NV)>(); break;
+          case 1: vm_wait<NS < 2 ? 0 : F::NV + F::NK + F::NV>(); break;
+          case 2: vm_wait<NS < 3 ? 0 : F::NV + 2 * (F::NK + F::NV)>(); break;
+          default: vm_wait<NS < 4 ? 0 : F::NV + 3 * (F::NK + F::NV)>(); break;
         }
         f32x4 s[RB][2];
 #pragma unroll
@@ -330,8 +332,8 @@ __global__ void __launch_bounds__(256, 2) k_paged_few(PagedArgs a) {
           switch (left) {
             case 0: vm_wait<0>(); break;
             case 1: vm_wait<F::NK + F::NV>(); break;
-            case 2: vm_wait<2 * (F::NK + F::NV)>(); break;
-            default: vm_wait<3 * (F::NK + F::NV)>(); break;
+            case 2: vm_wait<NS < 3 ? 0 : 2 * (F::NK + F::NV)>(); break;
+            default: vm_wait<NS < 4 ? 0 : 3 * (F::NK + F::NV)>(); break;
           }
         }
         bool odd = false;
@@ -831,6 +833,8 @@ void launch_few_format(const PagedArgs& a, hipStream_t s) {
 void launch_paged_mfma(const PagedArgs& a, int rows, hipStream_t s) {
   if (rows == MT_ROWS)
     a.c.head_dim == 128 ? launch_many<128>(a, s) : launch_many<64>(a, s);
+  else if (a.c.head_dim == 256)
+    rows == 16 ? launch_few_format<256, 1>(a, s) : launch_few_format<256, 2>(a, s);
   else if (a.c.head_dim == 128)
     rows == 16 ? launch_few_format<128, 1>(a, s) : launch_few_format<128, 2>(a, s);
   else

@@ -78,7 +78,7 @@ class Batch:
         rel = 2 * ds + 2.0 ** -22 + (n + 64) * 2.0 ** -24
         half = torch.finfo(self.dtype).eps / 2
         # on the bf16 matrix instruction the probabilities (with the values' scales) are rounded to bf16: 2^-8 each
-        low = 2.0 ** -8 if self.dtype == torch.bfloat16 and dh in (64, 128) and self.fmt != "f32" else 0.0
+        low = 2.0 ** -8 if self.dtype == torch.bfloat16 and dh in (64, 128, 256) and self.fmt != "f32" else 0.0
         assert (np.abs(o - want) <= (rel + low) * absum + half * np.abs(want) + 1e-30).all(), \
             (np.abs(o - want) - ((rel + low) * absum + half * np.abs(want))).max()
         some = np.isfinite(wl)
@@ -110,6 +110,22 @@ def test_page_sizes_and_windows(dtype, fmt, dh, size):
 @pytest.mark.parametrize("new,total", [(1, 4097), (1, 20000), (2, 9000), (300, 5000), (1030, 1030)])
 def test_long_sequences_are_cut_and_joined(dtype, fmt, new, total):
     Batch([(new, total)], 5, 1, 128, FORMATS[dtype], fmt, 64).check()
+
+
+@pytest.mark.parametrize("dtype,fmt", [("f32", "f32"), ("f32", "int8"), ("bf16", "f32"), ("bf16", "bf16"), ("bf16", "fp8")])
+@pytest.mark.parametrize("dh", [16, 48, 96, 112, 144, 240])
+def test_widths_between_the_kernels_own(dtype, fmt, dh):
+    b = Batch(RAGGED + [(33, 150)], 6, 2, dh, FORMATS[dtype], fmt, 12, seed=dh)
+    b.check()
+    b.check(window=40)
+
+
+@pytest.mark.parametrize("dtype,fmt", [("bf16", "bf16"), ("bf16", "fp8"), ("bf16", "int8"), ("f32", "bf16")])
+@pytest.mark.parametrize("seqs", [[(1, 5000)], [(2, 4000), (1, 1)], [(20, 900), (7, 2000)], [(300, 2000), (41, 41), (0, 9)]])
+def test_heads_of_256(dtype, fmt, seqs):
+    b = Batch(seqs, 8, 2, 256, FORMATS[dtype], fmt, 20, seed=3)
+    b.check()
+    b.check(window=333)
 
 
 @pytest.mark.parametrize("dtype,fmt", [("f32", "bf16"), ("bf16", "bf16"), ("bf16", "int8")])
