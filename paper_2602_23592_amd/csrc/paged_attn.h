@@ -219,7 +219,9 @@ typedef __attribute__((ext_vector_type(4))) float paged_f32x4;
 template <int TR>
 __device__ __forceinline__ void paged_finish(const PagedArgs& a, const PagedPlace& p, const PagedSeq& q, const PagedPart& part,
                                              int worker, const float* so, const float* sml) {
-  const int tid = threadIdx.x, row = tid % TR, quads = a.c.head_dim / 4;
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));  // (what follows from it is formed here, not kept in registers from job to job)
+  const int row = tid % TR, quads = a.c.head_dim / 4;
   const int x = p.tile * TR + row;
   const bool valid = x < q.rows * a.rep, whole = part.u0 == 0 && part.u1 == part.units;
   const int token = valid ? (int)div_by(x, a.by_rep) : 0, head = p.head * a.rep + (valid ? x - token * a.rep : 0);

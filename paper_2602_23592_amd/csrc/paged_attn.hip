@@ -97,10 +97,11 @@ __global__ void __launch_bounds__(256, ND <= 8 ? 2 : 1) k_paged_generic(PagedArg
   constexpr int TR = 16 * RB;
   extern __shared__ __attribute__((aligned(16))) float lds[];
   __shared__ int odd[2];  // some value of the tile (by turns) is not finite
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, g = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int dh = a.c.head_dim, nd = dh / 16;
   constexpr int stride = 16 * ND + 4;
-  const int worker = blockIdx.x;
+  // The workgroups of an XCD (blockIdx % 8) take neighbouring runs: one head's tiles read the same keys from its L2
+  const int worker = (blockIdx.x & 7) * (PAGED_WORKERS / 8) + (blockIdx.x >> 3);
   PagedSeq q;
   PagedPlace p = paged_place<TR, GT_KEYS>(a, worker, reinterpret_cast<uint64_t*>(lds), q);
   if (tid == 0) a.rec[worker].last = 0;
@@ -119,6 +120,9 @@ __global__ void __launch_bounds__(256, ND <= 8 ? 2 : 1) k_paged_generic(PagedArg
     int pos[RB], lo[RB];
     f32x4 qf[RB][ND], acc[RB][ND];
     float m[RB], l[RB];
+    int ln = lane;
+    asm volatile("" : "+v"(ln));  // (what follows from it is formed in every job, not kept in registers)
+    const int col = ln & 15, g = ln >> 4;
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
       const int x = p.tile * TR + 16 * b + col;
@@ -250,7 +254,7 @@ __global__ void __launch_bounds__(256, ND <= 8 ? 2 : 1) k_paged_generic(PagedArg
 // (8 jobs of 64 parts of 5 rows: 21 us with the parts along 8 lanes and two passes over them, 12 with 4096 workgroups of
 // which nearly all find no record, 7 with a wave for all of a job's parts, 4 like this.)
 template <int TR>
-__global__ void __launch_bounds__(512) k_paged_join(PagedArgs a, int groups) {
+__global__ void __launch_bounds__(512, 4) k_paged_join(PagedArgs a, int groups) {
   constexpr int RB = TR < 64 ? TR : 64;  // rows side by side in a wave
   __shared__ float s_m[8][RB], s_l[8][RB];
   __shared__ f32x4 s_o[8][4][RB];
