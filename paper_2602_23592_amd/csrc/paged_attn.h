@@ -204,14 +204,6 @@ __device__ __forceinline__ void paged_next(const PagedArgs& a, PagedPlace& p, Pa
   while (q.rows == 0 && p.seq + 1 < a.n_seqs);
 }
 
-// Element offset of key `key` of a sequence, head excluded
-__device__ __forceinline__ int64_t paged_key(const PagedArgs& a, const int32_t* table, int key, int64_t& scale) {
-  const int n = (int)div_by(key, a.by_page), at = key - n * a.c.page_size;
-  const int page = min(max(table[n], 0), a.c.n_pages - 1);
-  scale = (int64_t)page * a.c.n_kv_heads * a.c.page_size + at;
-  return page * a.c.page_stride + at * a.c.token_stride;
-}
-
 typedef __attribute__((ext_vector_type(4))) float paged_f32x4;
 
 // The four waves' parts of a job (each of other keys), added in their order: the job's result, or a partial one where the job

@@ -4,6 +4,7 @@
 // One pass over the keys with a running maximum m and sum l per query row (log2 domain):
 //   m' = max(m, s),  l' = l 2^(m - m') + sum 2^(s - m'),  O' = O 2^(m - m') + 2^(s - m') V,   result O / l.
 #include <algorithm>
+#include <type_traits>
 
 #include "paged_attn.h"
 
@@ -49,38 +50,46 @@ __device__ __forceinline__ bool finite4(f32x4 v) {
 // A thread's share of a key tile: every fourth four values of one key
 template <int ND>
 struct GenericShare {
-  int64_t at, scale_at;  // -1: behind the sequence's end
+  int64_t at, scale_at;  // of the tile on its way; -1: the key lies behind the sequence's end
+  int page;              // of the key in the tile after that (a tile's loads would else wait for their page's)
   uint4 raw[ND];
   float scale;
 };
 template <int ND>
+__device__ __forceinline__ void generic_page(const PagedArgs& a, const PagedSeq& q, const int32_t* table, int kt,
+                                             GenericShare<ND>& f) {
+  const int key = kt * GT_KEYS + (int)(threadIdx.x >> 2);
+  if (key < q.len) f.page = table[div_by(key, a.by_page)];
+}
+template <int ND>
 __device__ __forceinline__ void generic_locate(const PagedArgs& a, const PagedPlace& p, const PagedSeq& q, const int32_t* table,
                                                int kt, GenericShare<ND>& f) {
-  const int key = kt * GT_KEYS + (threadIdx.x >> 2);
+  const int key = kt * GT_KEYS + (int)(threadIdx.x >> 2);
   f.at = -1;
   if (key >= q.len) return;
-  f.at = paged_key(a, table, key, f.scale_at) + p.head * a.c.head_stride + (threadIdx.x & 3) * 4;
-  f.scale_at += (int64_t)p.head * a.c.page_size;
+  const int page = min(max(f.page, 0), a.c.n_pages - 1), in = key - (int)div_by(key, a.by_page) * a.c.page_size;
+  f.at = page * a.c.page_stride + in * a.c.token_stride + p.head * a.c.head_stride + (threadIdx.x & 3) * 4;
+  f.scale_at = ((int64_t)page * a.c.n_kv_heads + p.head) * a.c.page_size + in;
+  generic_page(a, q, table, kt + 1, f);
 }
 template <int FORMAT, int ND>
 __device__ __forceinline__ void generic_load(const PagedArgs& a, const void* values, const float* scales, GenericShare<ND>& f) {
+  const bool there = f.at >= 0;
   f.scale = 1.f;
+  if (FORMAT == KEEP_CACHE_FP8 || FORMAT == KEEP_CACHE_INT8) f.scale = scales[there ? f.scale_at : 0];
+  const int64_t at = there ? f.at : 0;  // (a place that may be read)
 #pragma unroll
-  for (int j = 0; j < ND; ++j) f.raw[j] = make_uint4(0, 0, 0, 0);
-  if (f.at < 0) return;
-  if (FORMAT == KEEP_CACHE_FP8 || FORMAT == KEEP_CACHE_INT8) f.scale = scales[f.scale_at];
-#pragma unroll
-  for (int j = 0; j < ND; ++j)
-    if (16 * j < a.c.head_dim) f.raw[j] = load_raw<FORMAT>(values, f.at + 16 * j);
+  for (int j = 0; j < ND; ++j) f.raw[j] = load_raw<FORMAT>(values, at + min(16 * j, a.c.head_dim - 16));
 }
 // ... to LDS; returns whether all are finite
 template <int FORMAT, int ND>
-__device__ __forceinline__ bool generic_store(float* tile, const GenericShare<ND>& f) {
+__device__ __forceinline__ bool generic_store(float* tile, int head_dim, const GenericShare<ND>& f) {
   float* to = tile + (threadIdx.x >> 2) * (16 * ND + 4) + (threadIdx.x & 3) * 4;
   bool ok = true;
 #pragma unroll
   for (int j = 0; j < ND; ++j) {
-    const f32x4 v = value_of<FORMAT>(f.raw[j], f.scale);
+    const bool there = f.at >= 0 && 16 * j < head_dim;
+    const f32x4 u = value_of<FORMAT>(f.raw[j], f.scale), v = there ? u : f32x4{0.f, 0.f, 0.f, 0.f};
     ok = ok && finite4(v);
     *reinterpret_cast<f32x4*>(to + 16 * j) = v;
   }
@@ -115,8 +124,7 @@ __global__ void __launch_bounds__(256, ND <= 8 ? 2 : 1) k_paged_generic(PagedArg
     const int32_t* table = a.table + (int64_t)p.seq * a.max_pages;
     const int kt1 = part.first + part.u1;
     GenericShare<ND> next;
-    generic_locate(a, p, q, table, part.first + part.u0, next);
-    generic_load<FORMAT>(a, a.c.k, a.c.k_scale, next);
+    generic_page(a, q, table, part.first + part.u0, next);
     int pos[RB], lo[RB];
     f32x4 qf[RB][ND], acc[RB][ND];
     float m[RB], l[RB];
@@ -131,35 +139,52 @@ __global__ void __launch_bounds__(256, ND <= 8 ? 2 : 1) k_paged_generic(PagedArg
       const int head = p.head * a.rep + (valid ? x - token * a.rep : 0);
       pos[b] = valid ? q.len - q.rows + token : -1;
       lo[b] = a.window ? max(0, pos[b] - a.window + 1) : 0;
-      const int64_t q_at = (int64_t)(q.row0 + token) * a.q_stride + (int64_t)head * dh + g * 4 * ND;
-#pragma unroll
-      for (int i = 0; i < ND; ++i) qf[b][i] = acc[b][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      const int64_t q_at = (int64_t)(q.row0 + token) * a.q_stride + (int64_t)head * dh;
+      // (behind the head's width: zeros, read from a place that may be read)
       if (a.dtype == KEEP_F32) {
 #pragma unroll
         for (int i = 0; i < ND; ++i)
-          if (g * 4 * ND + 4 * i < dh) qf[b][i] = value_of<KEEP_CACHE_F32>(load_raw<KEEP_CACHE_F32>(a.q, q_at + 4 * i), 1.f);
+          qf[b][i] = value_of<KEEP_CACHE_F32>(load_raw<KEEP_CACHE_F32>(a.q, q_at + min(g * 4 * ND + 4 * i, dh - 4)), 1.f);
       } else {
 #pragma unroll
         for (int i = 0; i < ND; ++i)
-          if (g * 4 * ND + 4 * i < dh) qf[b][i] = value_of<KEEP_CACHE_BF16>(load_raw<KEEP_CACHE_BF16>(a.q, q_at + 4 * i), 1.f);
+          qf[b][i] = value_of<KEEP_CACHE_BF16>(load_raw<KEEP_CACHE_BF16>(a.q, q_at + min(g * 4 * ND + 4 * i, dh - 4)), 1.f);
+      }
+#pragma unroll
+      for (int i = 0; i < ND; ++i) {
+        if (g * 4 * ND + 4 * i >= dh) qf[b][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        acc[b][i] = f32x4{0.f, 0.f, 0.f, 0.f};
       }
       m[b] = -INFINITY;
       l[b] = 0.f;
     }
+    generic_locate(a, p, q, table, part.first + part.u0, next);
+    generic_load<FORMAT>(a, a.c.k, a.c.k_scale, next);
     __syncthreads();  // the LDS of the division, or of the job before, has been read
     if (tid == 0) odd[0] = odd[1] = 0;
-    for (int kt = part.first + part.u0; kt < kt1; ++kt) {
+    int min_pos, max_lo;  // over the tile's rows
+    {
+      const int x1 = min(q.rows * a.rep, (p.tile + 1) * TR) - 1;
+      min_pos = q.len - q.rows + (int)div_by(p.tile * TR, a.by_rep);
+      max_lo = a.window ? max(0, q.len - q.rows + (int)div_by(x1, a.by_rep) - a.window + 1) : 0;
+    }
+    // One key tile; MASKED: some row does not see some key of it
+    const auto tile = [&](int kt, auto masked_type) __attribute__((always_inline)) {
+      constexpr bool MASKED = decltype(masked_type)::value;
       const int turn = (kt - part.first - part.u0) & 1;
-      generic_store<FORMAT>(sk, next);
+      generic_store<FORMAT>(sk, dh, next);
       __syncthreads();
       generic_load<FORMAT>(a, a.c.v, a.c.v_scale, next);
       const float* wk = sk + (wave * 16 + col) * stride + g * 4 * ND;
       f32x4 s[RB];
 #pragma unroll
       for (int b = 0; b < RB; ++b) s[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+      f32x4 ahead = *reinterpret_cast<const f32x4*>(wk);
 #pragma unroll
       for (int i = 0; i < ND; ++i) {
-        const f32x4 k = *reinterpret_cast<const f32x4*>(wk + 4 * i);
+        const f32x4 k = ahead;
+        if (i + 1 < ND) ahead = *reinterpret_cast<const f32x4*>(wk + 4 * i + 4);
+        __builtin_amdgcn_sched_barrier(0);  // (one operand ahead: all of them would push registers out to memory)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
@@ -172,7 +197,7 @@ __global__ void __launch_bounds__(256, ND <= 8 ? 2 : 1) k_paged_generic(PagedArg
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int key = key0 + 4 * g + r;
-          s[b][r] = key <= pos[b] && key >= lo[b] ? s[b][r] * a.scale_log2e : -INFINITY;
+          s[b][r] = !MASKED || (key <= pos[b] && key >= lo[b]) ? s[b][r] * a.scale_log2e : -INFINITY;
           top = fmaxf(top, s[b][r]);
         }
         top = fmaxf(top, __shfl_xor(top, 16, 64));
@@ -191,7 +216,8 @@ __global__ void __launch_bounds__(256, ND <= 8 ? 2 : 1) k_paged_generic(PagedArg
           l[b] += s[b][r];
         }
       }
-      if (!generic_store<FORMAT>(sv, next)) odd[turn] = 1;
+      const bool ok = generic_store<FORMAT>(sv, dh, next);
+      if (MASKED && !ok) odd[turn] = 1;
       __syncthreads();
       if (tid == 0) odd[turn ^ 1] = 0;
       if (kt + 1 < kt1) {
@@ -199,15 +225,27 @@ __global__ void __launch_bounds__(256, ND <= 8 ? 2 : 1) k_paged_generic(PagedArg
         generic_load<FORMAT>(a, a.c.k, a.c.k_scale, next);
       }
       const float* wv = sv + (wave * 16) * stride;
-      if (!odd[turn]) {
+      if (!MASKED || !odd[turn]) {
+        constexpr int SOME = ND < 8 ? ND : 4;
+        float ahead_v[SOME];
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+        for (int i = 0; i < SOME; ++i) ahead_v[i] = wv[4 * g * stride + 16 * i + col];
 #pragma unroll
-          for (int i = 0; i < ND; ++i) {
-            const float v = wv[(4 * g + r) * stride + 16 * i + col];
+        for (int n = 0; n < 4 * ND / SOME; ++n) {
+          const int r = n * SOME / ND, i0 = n * SOME % ND, n1 = n + 1, r1 = n1 * SOME / ND, i1 = n1 * SOME % ND;
+          float v[SOME];
 #pragma unroll
-            for (int b = 0; b < RB; ++b) acc[b][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, s[b][r], acc[b][i], 0, 0, 0);
+          for (int i = 0; i < SOME; ++i) {
+            v[i] = ahead_v[i];
+            if (r1 < 4) ahead_v[i] = wv[(4 * g + r1) * stride + 16 * (i1 + i) + col];
           }
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int i = 0; i < SOME; ++i)
+#pragma unroll
+            for (int b = 0; b < RB; ++b)
+              acc[b][i0 + i] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[i], s[b][r], acc[b][i0 + i], 0, 0, 0);
+        }
       } else {
         // a product with a probability of zero would carry infinities and NaN to rows that do not see the key
 #pragma unroll 1
@@ -221,10 +259,17 @@ __global__ void __launch_bounds__(256, ND <= 8 ? 2 : 1) k_paged_generic(PagedArg
               const f32x4 v = *reinterpret_cast<const f32x4*>(wv + j * stride + 16 * i + 4 * g);
 #pragma unroll
               for (int e = 0; e < 4; ++e) acc[b][i][e] += sees ? pj * v[e] : 0.f;
+              __builtin_amdgcn_sched_barrier(0);  // (one read at a time: this path must not cost the other registers)
             }
           }
         }
       }
+    };
+    // Two loops, so that what masks need takes no registers from the tiles without: they are nearly all of them
+    const auto is_masked = [&](int kt) { return kt * GT_KEYS + GT_KEYS - 1 > min_pos || kt * GT_KEYS < max_lo; };
+    for (int kt = part.first + part.u0; kt < kt1;) {
+      for (; kt < kt1 && !is_masked(kt); ++kt) tile(kt, std::false_type{});
+      for (; kt < kt1 && is_masked(kt); ++kt) tile(kt, std::true_type{});
     }
 
     // ---- the four waves' parts, in their order
