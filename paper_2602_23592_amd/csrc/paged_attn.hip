@@ -527,7 +527,15 @@ extern "C" keep_status keep_paged_attention(const keep_paged_attention_desc* d, 
   // 59 / 56 / 64, 89 / 67 / 75.  Up to 16 rows a tile of 32 has nothing to gain.
   const bool mfma = d->dtype == KEEP_BF16 && has_mfma(cache);
   const int64_t mean = (d->n_rows * (int64_t)a.rep + d->n_seqs - 1) / d->n_seqs;
-  const int rows = mean <= 16 || (!mfma && cache->head_dim > 128) ? 16 : !mfma || mean <= 48 || cache->head_dim > 128 ? 32 : 128;
+  int rows = mean <= 16 ? 16 : 32;
+  if (mfma && cache->head_dim <= 128) {
+    if (mean > 48) rows = 128;
+  } else if (!mfma) {
+    // The fp32 kernel has no tiles of 32 rows above heads of 128 (registers), and where tiles of 32 rows would not give every worker
+    // two units, smaller tiles end sooner
+    const int64_t units = (d->n_rows * (int64_t)a.rep / 32 + d->n_seqs) * cache->n_kv_heads * (a.capacity / 64 + 1);
+    if (cache->head_dim > 128 || units < 2 * PAGED_WORKERS) rows = 16;
+  }
   a.part_o = a.part_ml + (size_t)2 * PAGED_WORKERS * 2 * rows;
   if (mfma)
     launch_paged_mfma(a, rows, static_cast<hipStream_t>(stream));
