@@ -81,7 +81,8 @@ __device__ __forceinline__ void store8(bf16_t* p, const float (&v)[8]) {
       make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
 }
 
-// Codes of eight values that are at most Q in magnitude.  v_cvt_pk_fp8_f32 rounds to the nearest even code.
+// Codes of eight values that are at most Q in magnitude, the nearest even ones: v_cvt_pk_fp8_f32 rounds so, and so does adding
+// 1.5 * 2^23, which leaves the integer in the sum's lowest bits.
 template <int FMT>
 __device__ __forceinline__ uint2 encode8(const float (&v)[8]) {
   uint32_t w[2];
@@ -91,9 +92,11 @@ __device__ __forceinline__ uint2 encode8(const float (&v)[8]) {
       int u = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i], v[4 * i + 1], 0, false);
       w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i + 2], v[4 * i + 3], u, true);
     } else {
-      w[i] = 0;
+      uint32_t u[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) w[i] |= ((uint32_t)(int)rintf(v[4 * i + e]) & 255u) << (8 * e);
+      for (int e = 0; e < 4; ++e) u[e] = __float_as_uint(v[4 * i + e] + 12582912.f);
+      const uint32_t lo = __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0400u), hi = __builtin_amdgcn_perm(u[3], u[2], 0x0c0c0400u);
+      w[i] = lo | hi << 16;
     }
   }
   return make_uint2(w[0], w[1]);
@@ -152,9 +155,22 @@ __device__ __forceinline__ void put8(void* pages, float* scales, const Place& p,
     for (int o = group >> 1; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
     const bool finite = top < 0x7f800000u;
     const float scale = finite ? fmaxf(__uint_as_float(top) * (1.f / Q), 1.17549435e-38f) : __uint_as_float(0x7fc00000u);
+    // The quotients by one reciprocal y = 1 / scale (rounded): q0 = x y is within 1.5 ulp, q1 = q0 + (x - q0 scale) y within one,
+    // so that the next remainder is exact and q2 = q1 + (x - q1 scale) y is x / scale as a division rounds it (Markstein's
+    // theorem), where nothing is lost to underflow: a remainder is a multiple of 2^-47 |q| scale, so from scale = 2^-64 on only
+    // quotients below 2^-38 could differ, and their code is zero.
     float u[8];
+    if (scale >= 5.421010862427522e-20f) {
+      const float y = 1.f / scale;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) u[e] = finite ? fminf(fmaxf(v[e] / scale, -Q), Q) : 0.f;
+      for (int e = 0; e < 8; ++e) {
+        const float q0 = v[e] * y, q1 = __builtin_fmaf(__builtin_fmaf(-q0, scale, v[e]), y, q0);
+        u[e] = __builtin_amdgcn_fmed3f(__builtin_fmaf(__builtin_fmaf(-q1, scale, v[e]), y, q1), -Q, Q);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) u[e] = finite ? fminf(fmaxf(v[e] / scale, -Q), Q) : 0.f;
+    }
     if (p.live) {
       *reinterpret_cast<uint2*>(static_cast<uint8_t*>(pages) + p.value) = encode8<FMT>(u);
       if (p.d == 0) scales[p.scale] = scale;

@@ -149,3 +149,26 @@ def test_binding_refuses():
                 (rows[:, :, :32], rows[:, :, :32], s), (rows, rows, s.long()), (rows.cpu(), rows.cpu(), s)):
         with pytest.raises(kb.KeepError):
             c.write(*bad)
+
+
+@pytest.mark.parametrize("fmt", ["fp8", "int8"])
+def test_quotients_beside_a_border_between_codes(fmt):
+    """x / scale next to every border between two codes, for scales over the whole range: codes as a division gives them"""
+    r = np.random.default_rng(17)
+    n, dh = 4096, 128
+    q = so.TOP[fmt]
+    edge = np.arange(127) + 0.5 if fmt == "int8" else np.unique(np.abs(np.concatenate(
+        [(a[:-1] + a[1:]) / 2 for a in [np.sort(torch.arange(127, dtype=torch.uint8).view(torch.float8_e4m3fn).float().numpy())]])))
+    x = np.empty((2, n, 1, dh), np.float32)
+    x[..., 0] = np.exp2(r.uniform(-126, 120, (2, n, 1))) * r.uniform(1, 2, (2, n, 1))      # the head's largest
+    x[..., 0].flat[:64] = 1e-45 * np.arange(64)
+    scale = np.maximum(x[..., :1] * np.float32(1) / np.float32(q), np.float32(2.0 ** -126)).astype(np.float64)
+    x[..., 1:] = (r.choice(edge, (2, n, 1, dh - 1)) * scale * (1 + r.integers(-3, 4, (2, n, 1, dh - 1)) * 2.0 ** -24)
+                  * r.choice([-1, 1], (2, n, 1, dh - 1)))
+    x[..., 1:] = np.clip(x[..., 1:], -np.abs(x[..., :1]), np.abs(x[..., :1]))
+    c = make(fmt, n // 16, 16, 1, dh)
+    c.write(torch.from_numpy(x[0]).cuda(), torch.from_numpy(x[1]).cuda(), torch.arange(n, dtype=torch.int32).cuda())
+    for got, scales, rows in ((c.k, c.k_scale, x[0]), (c.v, c.v_scale, x[1])):
+        want, s = so.quantise(rows, fmt)
+        assert np.array_equal(scales.cpu().numpy().reshape(n, 1), s)
+        assert np.array_equal(as_numbers(got).reshape(n, 1, dh), want)
