@@ -101,6 +101,11 @@ __device__ __forceinline__ bool generic_store(float* tile, int head_dim, const G
 // query row (lane % 16) of each 16 and four keys (4 (lane / 16) + r), which is the operand that O^T = V^T . P^T wants from it in
 // step r: the probabilities never leave their registers.  Rows of K and V in LDS are padded by four values, so that both operand
 // reads meet all banks.  V is on its way to registers while the scores are formed, the next tile's K during the second product.
+// Many rows: the fp32 matrix instruction is the bound, at half to two thirds of its rate (chunks of up to 2000 tokens over up to
+// 16k, heads of 80: 90 TFLOP/s, 128: 67, over an 8-bit cache 98; a large product 154): the barriers of a tile and, with fp32 keys of
+// 128, registers.  Few rows: HBM (64 tokens over up to 8k fp32 keys 359 us, 5.5 TB/s; one over 33k 65 us).  Staged without the
+// loads ahead, with an index for every value: 24 TFLOP/s and 2.1 TB/s.  16 rows to a tile instead of 32 read the keys twice as
+// often (24.2 ms against 10.3 for the chunks with heads of 128 before the loads were in this order).
 template <int FORMAT, int ND, int RB>
 __global__ void __launch_bounds__(256, ND <= 8 ? 2 : 1) k_paged_generic(PagedArgs a) {
   constexpr int TR = 16 * RB;
@@ -296,8 +301,9 @@ __global__ void __launch_bounds__(256, ND <= 8 ? 2 : 1) k_paged_generic(PagedArg
 // of, and `groups` times 16 of the output's dimensions (blockIdx.y).  Lanes lie along query rows, then along parts, and as many
 // waves as there are to spare for 16 dimensions along parts again, each lane with a running maximum and sum of its own, so that all
 // loads are independent of one another; a butterfly adds the lanes of a row, LDS the waves.
-// (8 jobs of 64 parts of 5 rows: 21 us with the parts along 8 lanes and two passes over them, 12 with 4096 workgroups of
-// which nearly all find no record, 7 with a wave for all of a job's parts, 4 like this.)
+// A chain of three reads that each wait for the one before (records, record, parts) bounds it.  8 jobs of 64 parts of 5 rows: 17 us
+// more with the parts along 8 lanes and two passes over them, 8 more with 4096 workgroups of which nearly all find no record, 3
+// more with a wave for all of a job's parts.  512 jobs: 8 us, 10 with registers for one workgroup per CU only.
 template <int TR>
 __global__ void __launch_bounds__(512, 4) k_paged_join(PagedArgs a, int groups) {
   constexpr int RB = TR < 64 ? TR : 64;  // rows side by side in a wave
@@ -533,7 +539,7 @@ extern "C" keep_status keep_paged_attention(const keep_paged_attention_desc* d, 
   } else if (!mfma) {
     // The fp32 kernel has no tiles of 32 rows above heads of 128 (registers), and where tiles of 32 rows would not give every worker
     // two units, smaller tiles end sooner
-    const int64_t units = (d->n_rows * (int64_t)a.rep / 32 + d->n_seqs) * cache->n_kv_heads * (a.capacity / 64 + 1);
+    const double units = (d->n_rows * (double)a.rep / 32 + d->n_seqs) * cache->n_kv_heads * (a.capacity / 64 + 1);
     if (cache->head_dim > 128 || units < 2 * PAGED_WORKERS) rows = 16;
   }
   a.part_o = a.part_ml + (size_t)2 * PAGED_WORKERS * 2 * rows;

