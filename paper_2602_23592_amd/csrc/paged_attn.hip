@@ -102,10 +102,9 @@ __device__ __forceinline__ bool generic_store(float* tile, int head_dim, const G
 // step r: the probabilities never leave their registers.  Rows of K and V in LDS are padded by four values, so that both operand
 // reads meet all banks.  V is on its way to registers while the scores are formed, the next tile's K during the second product.
 // Many rows: the fp32 matrix instruction is the bound, at half to two thirds of its rate (chunks of up to 2000 tokens over up to
-// 16k, heads of 80: 90 TFLOP/s, 128: 67, over an 8-bit cache 98; a large product 154): the barriers of a tile and, with fp32 keys of
-// 128, registers.  Few rows: HBM (64 tokens over up to 8k fp32 keys 359 us, 5.5 TB/s; one over 33k 65 us).  Staged without the
-// loads ahead, with an index for every value: 24 TFLOP/s and 2.1 TB/s.  16 rows to a tile instead of 32 read the keys twice as
-// often (24.2 ms against 10.3 for the chunks with heads of 128 before the loads were in this order).
+// 16k, heads of 80: 90 TFLOP/s, 128: 72, over an 8-bit cache 98; a large product 154): the barriers of a tile, which two waves
+// per SIMD do not hide.  Few rows: HBM (64 tokens over up to 8k fp32 keys 359 us, 5.5 TB/s; one over 33k 65 us).  Staged without
+// the loads ahead, with an index for every value: 24 TFLOP/s and 2.1 TB/s.
 template <int FORMAT, int ND, int RB>
 __global__ void __launch_bounds__(256, ND <= 8 ? 2 : 1) k_paged_generic(PagedArgs a) {
   constexpr int TR = 16 * RB;
@@ -255,17 +254,18 @@ __global__ void __launch_bounds__(256, ND <= 8 ? 2 : 1) k_paged_generic(PagedArg
         // a product with a probability of zero would carry infinities and NaN to rows that do not see the key
 #pragma unroll 1
         for (int j = 0; j < 16; ++j) {
+          float pj[RB];
 #pragma unroll
-          for (int b = 0; b < RB; ++b) {
-            const float pj = __shfl(j & 2 ? j & 1 ? s[b][3] : s[b][2] : j & 1 ? s[b][1] : s[b][0], (j >> 2) * 16 + col, 64);
-            const bool sees = key0 + j <= pos[b] && key0 + j >= lo[b];
+          for (int b = 0; b < RB; ++b)
+            pj[b] = __shfl(j & 2 ? j & 1 ? s[b][3] : s[b][2] : j & 1 ? s[b][1] : s[b][0], (j >> 2) * 16 + col, 64);
 #pragma unroll
-            for (int i = 0; i < ND; ++i) {
-              const f32x4 v = *reinterpret_cast<const f32x4*>(wv + j * stride + 16 * i + 4 * g);
+          for (int i = 0; i < ND; ++i) {
+            const f32x4 v = *reinterpret_cast<const f32x4*>(wv + j * stride + 16 * i + 4 * g);
 #pragma unroll
-              for (int e = 0; e < 4; ++e) acc[b][i][e] += sees ? pj * v[e] : 0.f;
-              __builtin_amdgcn_sched_barrier(0);  // (one read at a time: this path must not cost the other registers)
-            }
+            for (int b = 0; b < RB; ++b)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) acc[b][i][e] += key0 + j <= pos[b] && key0 + j >= lo[b] ? pj[b] * v[e] : 0.f;
+            __builtin_amdgcn_sched_barrier(0);  // (one read at a time: this path must not cost the other registers)
           }
         }
       }
@@ -430,14 +430,21 @@ static void launch_generic(const PagedArgs& a, hipStream_t s) {
   hipLaunchKernelGGL((k_paged_generic<FORMAT, ND, RB>), dim3(PAGED_WORKERS), dim3(256), lds, s, a);
   launch_paged_join(a, 16 * RB, s);
 }
+// Whether tiles of 32 query rows have the registers: with fp32 keys of 128 they would spill (us on tiles of 16 / 32: one sequence of
+// 33k keys with 20 rows 87 / 113, eight chunks 8193 / 8764, but 64 sequences of up to 8k keys with 20 rows 630 / 587).
+constexpr bool paged_wide_tiles(int format, int head_dim) { return head_dim <= (format == KEEP_CACHE_F32 ? 80 : 128); }
+
 template <int FORMAT>
 static void launch_generic(const PagedArgs& a, int rows, hipStream_t s) {
   const int dh = a.c.head_dim;
   if (rows == 16)
-    dh <= 64 ? launch_generic<FORMAT, 4, 1>(a, s) : dh <= 80 ? launch_generic<FORMAT, 5, 1>(a, s)
-    : dh <= 128 ? launch_generic<FORMAT, 8, 1>(a, s) : launch_generic<FORMAT, 16, 1>(a, s);
-  else
-    dh <= 64 ? launch_generic<FORMAT, 4, 2>(a, s) : dh <= 80 ? launch_generic<FORMAT, 5, 2>(a, s) : launch_generic<FORMAT, 8, 2>(a, s);
+    return dh <= 64    ? launch_generic<FORMAT, 4, 1>(a, s)
+           : dh <= 80  ? launch_generic<FORMAT, 5, 1>(a, s)
+           : dh <= 128 ? launch_generic<FORMAT, 8, 1>(a, s)
+                       : launch_generic<FORMAT, 16, 1>(a, s);
+  if (dh <= 64) return launch_generic<FORMAT, 4, 2>(a, s);
+  if (dh <= 80) return launch_generic<FORMAT, 5, 2>(a, s);
+  if constexpr (paged_wide_tiles(FORMAT, 128)) launch_generic<FORMAT, 8, 2>(a, s);
 }
 
 void launch_paged_generic(const PagedArgs& a, int rows, hipStream_t s) {
@@ -537,10 +544,12 @@ extern "C" keep_status keep_paged_attention(const keep_paged_attention_desc* d, 
   if (mfma && cache->head_dim <= 128) {
     if (mean > 48) rows = 128;
   } else if (!mfma) {
-    // The fp32 kernel has no tiles of 32 rows above heads of 128 (registers), and where tiles of 32 rows would not give every worker
-    // two units, smaller tiles end sooner
+    // The fp32 kernel has no tiles of 32 rows where their registers do not fit (paged_wide_tiles), and where such tiles would not
+    // give every worker two units, smaller ones end sooner (three short sequences with heads of 64: 10.4 us instead of 12.6).
+    // Else us on tiles of 16 / 32, 64 sequences of up to 8k 8-bit keys with 20 and 60 rows: 449 / 357, 883 / 698; one of 33k with
+    // 125 rows: 242 / 201; eight chunks of up to 2000 tokens: 7671 / 6052.
     const double units = (d->n_rows * (double)a.rep / 32 + d->n_seqs) * cache->n_kv_heads * (a.capacity / 64 + 1);
-    if (cache->head_dim > 128 || units < 2 * PAGED_WORKERS) rows = 16;
+    if (!paged_wide_tiles(cache->format, cache->head_dim) || units < 2 * PAGED_WORKERS) rows = 16;
   }
   a.part_o = a.part_ml + (size_t)2 * PAGED_WORKERS * 2 * rows;
   if (mfma)
