@@ -260,8 +260,8 @@ __device__ __forceinline__ void paged_finish(const PagedArgs& a, const PagedPlac
 }
 
 void launch_paged_generic(const PagedArgs& a, int rows, hipStream_t s);  // tiles of 16 or 32 query rows
-// bf16 queries, heads of 64, 128 or 256, a bf16 or 8-bit cache of less than 64 GB per tensor; rows: query rows of a tile (16, 32
-// or, up to heads of 128, 128)
+// bf16 queries, heads of 64, 128 or 256, a bf16 or 8-bit cache of less than 64 GB per tensor; rows: query rows of a tile (16, 32 or
+// 128; heads of 256 16, with bf16 keys 32 too)
 void launch_paged_mfma(const PagedArgs& a, int rows, hipStream_t s);
 void launch_paged_join(const PagedArgs& a, int rows, hipStream_t s);
 

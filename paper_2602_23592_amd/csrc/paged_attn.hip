@@ -541,9 +541,14 @@ extern "C" keep_status keep_paged_attention(const keep_paged_attention_desc* d, 
   const bool mfma = d->dtype == KEEP_BF16 && has_mfma(cache);
   const int64_t mean = (d->n_rows * (int64_t)a.rep + d->n_seqs - 1) / d->n_seqs;
   int rows = mean <= 16 ? 16 : 32;
-  if (mfma && cache->head_dim <= 128) {
+  if (mfma && cache->head_dim == 256) {
+    // (heads of 256: a workgroup per CU with bf16 keys or 32 rows.  us on tiles of 16 / 32: 64 sequences of up to 8k 8-bit keys with
+    // 32 rows 58 / 104, eight chunks 937 / 1432; bf16, 32, 128, 512 and 2048 rows 99 / 122, 262 / 257, 931 / 819, 3699 / 3286,
+    // one sequence of 33k keys with 512 and 8000 rows 119 / 134, 2462 / 1257)
+    rows = cache->format == KEEP_CACHE_BF16 && mean > 512 ? 32 : 16;
+  } else if (mfma) {
     if (mean > 48) rows = 128;
-  } else if (!mfma) {
+  } else {
     // The fp32 kernel has no tiles of 32 rows where their registers do not fit (paged_wide_tiles), and where such tiles would not
     // give every worker two units, smaller ones end sooner (three short sequences with heads of 64: 10.4 us instead of 12.6).
     // Else us on tiles of 16 / 32, 64 sequences of up to 8k 8-bit keys with 20 and 60 rows: 449 / 357, 883 / 698; one of 33k with

@@ -12,10 +12,17 @@
 // operands; a key's scale multiplies its scores, a value's scale its probability, in binary32.  Probabilities (with the
 // value's scale) are rounded to bf16 for the product, the row sums are taken before that.
 //
+// 64 sequences of one token with 40 / 8 heads of 128 over up to 8k keys in fp8 (512 MB): 111 us, 4.6 TB/s (and 8 for the join) where a
+// copy reaches 4.7; one token over 33k bf16 keys (135 MB): 33 us, 4.1 TB/s (and 9).  The first kernel, on the fp32 matrix
+// instruction with staging behind barriers, took 940 and 167.
+//
 // k_paged_many: tiles of 128 query rows, 32 per wave, over key tiles of 64 that the workgroup shares in LDS (two of them: the
 // next arrives while one is used), where the matrix instruction and the exponentials are the bound.  32x32x16: a lane owns a
 // query row (lane % 32) and half of the tile's keys, and again S^T = K . Q^T leaves the operand of O^T = V^T . P^T.
 // 8-bit codes become bf16 on their way into LDS, once for the four waves.
+// Eight chunks of 100 to 2000 tokens over up to 16k keys, 28 / 4 heads of 128, bf16 (589 GFLOP): 763 us, 772 TFLOP/s, where a large
+// product reaches 1419; 256 tokens over 33k int8 keys, 40 / 8 heads: 256 us, 673 TFLOP/s (bf16 10 % more).  Exponentials and
+// conversions share the SIMD with the products, and 32 rows per wave feed each K and V operand to one product only.
 #include <type_traits>
 
 #include "paged_attn.h"
@@ -831,10 +838,10 @@ void launch_few_format(const PagedArgs& a, hipStream_t s) {
 }  // namespace
 
 void launch_paged_mfma(const PagedArgs& a, int rows, hipStream_t s) {
-  if (rows == MT_ROWS)
+  if (a.c.head_dim == 256)
+    rows == 16 ? launch_few_format<256, 1>(a, s) : launch_few<256, KEEP_CACHE_BF16, 2>(a, s);
+  else if (rows == MT_ROWS)
     a.c.head_dim == 128 ? launch_many<128>(a, s) : launch_many<64>(a, s);
-  else if (a.c.head_dim == 256)
-    rows == 16 ? launch_few_format<256, 1>(a, s) : launch_few_format<256, 2>(a, s);
   else if (a.c.head_dim == 128)
     rows == 16 ? launch_few_format<128, 1>(a, s) : launch_few_format<128, 2>(a, s);
   else

@@ -128,6 +128,22 @@ def test_heads_of_256(dtype, fmt, seqs):
     b.check(window=333)
 
 
+@pytest.mark.parametrize("fmt", ["bf16", "fp8"])
+@pytest.mark.parametrize("seqs", [[(701, 1500)], [(200, 333), (199, 4100)]])
+def test_long_chunks_with_heads_of_256(fmt, seqs):
+    b = Batch(seqs, 6, 1, 256, torch.bfloat16, fmt, 24, seed=4)
+    b.check()
+    b.check(window=100)
+    new, total = seqs[0]
+    key = total - 130                                    # not finite: only the rows that see it may show that
+    (b.cache.v if fmt == "bf16" else b.cache.v_scale)[int(b.table[0, key // 24]), 0, key % 24] = float("nan")
+    out, _ = b.run(window=100)
+    sees = torch.zeros(out.shape[0], dtype=torch.bool, device="cuda")
+    sees[new - 130:new - 30] = True
+    end = int(b.start[-1])
+    assert torch.isnan(out[:end][sees[:end]]).all() and torch.isfinite(out[:end][~sees[:end]]).all()
+
+
 @pytest.mark.parametrize("dtype,fmt", [("f32", "bf16"), ("bf16", "bf16"), ("bf16", "int8")])
 def test_many_sequences(dtype, fmt):
     r = np.random.default_rng(5)
