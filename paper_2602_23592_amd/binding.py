@@ -348,6 +348,17 @@ def _launch(device: torch.device, stream, call, *args):
         raise KeepError(st, _lib.keep_last_error(None).decode())
 
 
+def _empty(shape, dtype: torch.dtype, device: torch.device, stream) -> torch.Tensor:
+    """New memory that belongs to the stream of the call: its next use there waits for the call, wherever the tensor is dropped"""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = _stream_handle(stream)
+        stream = torch.cuda.ExternalStream(handle, device=device) if handle else torch.cuda.default_stream(device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _array(name: str, t: Optional[torch.Tensor], dtype, numel: int, device: torch.device, optional: bool = False):
     """Address of a dense device array of `numel` elements"""
     if t is None:
@@ -471,7 +482,7 @@ def paged_attention(q: torch.Tensor, cache: PagedCache, q_start: torch.Tensor, k
                     page_table: torch.Tensor, window: int = 0, scale: float = 0.0, out: Optional[torch.Tensor] = None,
                     lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """keep_paged_attention: q [rows, n_q_heads, head_dim] of len(kv_len) sequences, rows q_start[s] .. q_start[s + 1] each,
-    page_table int32 [n_seqs, max_pages].  out and workspace (uint8) are allocated where they are not given."""
+    page_table int32 [n_seqs, max_pages].  out and workspace (uint8) are allocated where they are not given, for `stream`."""
     stride = _heads("q", q, cache.device)
     n, hq, d = q.shape
     if d != cache.c.head_dim:
@@ -480,12 +491,12 @@ def paged_attention(q: torch.Tensor, cache: PagedCache, q_start: torch.Tensor, k
     if page_table.dim() != 2 or page_table.shape[0] != seqs:
         _refuse("page_table must be [n_seqs, max_pages]")
     if out is None:
-        out = torch.empty((n, hq, d), dtype=q.dtype, device=q.device)
+        out = _empty((n, hq, d), q.dtype, q.device, stream)
     if out.shape != q.shape:
         _refuse("out must have the shape of q")
     need = paged_attention_workspace_bytes(hq, cache, seqs)
     if workspace is None:
-        workspace = torch.empty(max(1, need), dtype=torch.uint8, device=q.device)
+        workspace = _empty(max(1, need), torch.uint8, q.device, stream)
     desc = PagedAttentionDesc(_DTYPES[q.dtype], seqs, n, hq, page_table.shape[1], window, scale, stride,
                               _heads("out", out, q.device, q.dtype))
     dev = cache.device
@@ -512,9 +523,9 @@ def sample(logits: torch.Tensor, uniform: torch.Tensor, temperature: Optional[to
     n, vocab = logits.shape
     dev = logits.device
     if tokens is None:
-        tokens = torch.empty(n, dtype=torch.int32, device=dev)
+        tokens = _empty(n, torch.int32, dev, stream)
     if workspace is None:
-        workspace = torch.empty(max(1, sample_workspace_bytes(n, vocab)), dtype=torch.uint8, device=dev)
+        workspace = _empty(max(1, sample_workspace_bytes(n, vocab)), torch.uint8, dev, stream)
     desc = SampleDesc(_DTYPES[logits.dtype], n, vocab, logits.stride(0) if n > 1 else vocab)
     _launch(dev, stream, lib.keep_sample, C.byref(desc), logits.data_ptr(), _array("uniform", uniform, torch.float32, n, dev),
             _array("temperature", temperature, torch.float32, n, dev, True), _array("top_k", top_k, torch.int32, n, dev, True),

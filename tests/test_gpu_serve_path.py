@@ -203,3 +203,32 @@ def test_calls_on_other_streams_and_at_the_same_time():
         kb.sample(logits, u, tokens=outs[2], workspace=ws[2], stream=streams[2])
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+@pytest.mark.parametrize("as_handle", [False, True])
+def test_what_a_call_allocates_belongs_to_its_stream(as_handle):
+    """Results and workspaces of calls that wait on a busy stream, while the current one takes and fills memory of their sizes"""
+    hq, hkv, dh, n = 4, 2, 64, 3000
+    g = torch.Generator().manual_seed(6)
+    cache = kb.PagedCache.empty(torch.bfloat16, 190, 16, hkv, dh)
+    cache.write(torch.randn(n, hkv, dh, generator=g).bfloat16().cuda(), torch.randn(n, hkv, dh, generator=g).bfloat16().cuda(),
+                torch.arange(n, dtype=torch.int32, device="cuda"))
+    table = torch.arange(190, dtype=torch.int32, device="cuda")[None]
+    q = torch.randn(40, hq, dh, generator=g).bfloat16().cuda()
+    logits, u = torch.randn(3, 60000, generator=g).cuda(), torch.rand(3, generator=g).cuda()
+    args = (q, cache, i32([0, 40]), i32([n]), table)
+    want = [kb.paged_attention(*args), kb.sample(logits, u)]
+    sizes = [kb.paged_attention_workspace_bytes(hq, cache, 1), kb.sample_workspace_bytes(3, 60000), q.numel() * 2, 12]
+    a = torch.randn(4096, 4096, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        with torch.cuda.stream(side):
+            busy = a
+            for _ in range(20):
+                busy = a @ a
+        s = side.cuda_stream if as_handle else side
+        got = [kb.paged_attention(*args, stream=s), kb.sample(logits, u, stream=s)]
+        filled = [torch.full((size,), 255, dtype=torch.uint8, device="cuda") for size in sizes]
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(got, want)) and all((f == 255).all() for f in filled)
