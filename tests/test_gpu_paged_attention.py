@@ -72,7 +72,7 @@ class Batch:
         # A score is off by ds: dh products and sums of binary32 (2^-24 each, of sums of |q k| <= |q| |k|), the scale, the
         # 8-bit scale and the exponent's argument a few more.  A probability is off by 2 ds (its own and the norm's), 2^-22 of
         # the exponential; n of them are added (2^-24 each).
-        scale = kw.get("scale") or dh ** -0.5
+        scale = abs(kw.get("scale") or dh ** -0.5)
         qk = np.linalg.norm(q[:end], axis=-1).max(initial=0) * np.sqrt(np.nanmax(np.nansum(k * k, -1), initial=0)) * scale
         ds = (dh + 8) * 2.0 ** -24 * qk
         rel = 2 * ds + 2.0 ** -22 + (n + 64) * 2.0 ** -24
@@ -253,3 +253,11 @@ def test_binding_refuses():
                      ((b.q, b.cache, start, one, b.table), {"workspace": torch.zeros(512, dtype=torch.uint8, device="cuda")})):
         with pytest.raises(kb.KeepError):
             kb.paged_attention(*args, **kw)
+
+
+@pytest.mark.parametrize("dtype,fmt", [("f32", "f32"), ("f32", "fp8"), ("bf16", "bf16"), ("bf16", "fp8"), ("bf16", "int8")])
+@pytest.mark.parametrize("dh", [64, 80, 128, 256])
+def test_negative_scales(dtype, fmt, dh):
+    """a negative factor on every tile, where the largest product is not the largest score"""
+    for new in (1, 7, 20, 300):
+        Batch([(new, 700), (min(new, 4), 33)], 4, 2, dh, FORMATS[dtype], fmt, 16, seed=new).check(scale=-0.07)
