@@ -85,7 +85,8 @@ keep_status keep_rope_rows(const keep_rope_rows_desc* desc, const void* q_in, vo
  * The 8-bit formats keep one binary32 scale per token and head, of keys and of values:
  *   scale = max(largest magnitude of the head_dim values * (1 / Q), 2^-126),   code = value / scale, at most Q in magnitude,
  * rounded to the nearest even code (INT8: whole numbers, Q = 127; FP8: the 8-bit floats of 4 exponent and 3 mantissa bits,
- * Q = 448), each operation rounded to binary32; a code stands for code * scale.  A head with a value that is not finite is stored with the scale NaN and reads back as NaN throughout. */
+ * Q = 448), each operation rounded to binary32; a code stands for code * scale.  A head with a value that is not finite is
+ * stored with the scale NaN and reads back as NaN throughout. */
 typedef enum { KEEP_CACHE_F32 = 0, KEEP_CACHE_BF16 = 1, KEEP_CACHE_FP8 = 2, KEEP_CACHE_INT8 = 3 } keep_cache_format;
 
 typedef struct {
