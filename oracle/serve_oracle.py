@@ -84,10 +84,10 @@ def paged_attention(q, k_pages, v_pages, q_start, kv_len, table, window=0, scale
     out, absum = np.full((2, rows, hq, dh), np.nan)
     lse = np.full((rows, hq), np.nan)
     for s in range(len(kv_len)):
-        n = q_start[s + 1] - q_start[s]
+        n = int(q_start[s + 1] - q_start[s])
         k, v = gather(k_pages, table[s], kv_len[s]), gather(v_pages, table[s], kv_len[s])
         for i in range(n):
-            r, pos = q_start[s] + i, kv_len[s] - n + i
+            r, pos = q_start[s] + i, int(kv_len[s]) - n + i
             lo = max(0, pos - window + 1) if window else 0
             if pos < 0:
                 out[r], absum[r], lse[r] = 0, 0, -np.inf

@@ -62,18 +62,25 @@ __device__ __forceinline__ PagedSeq paged_uniform(PagedSeq q) {
   return PagedSeq{paged_uniform(q.row0), paged_uniform(q.rows), paged_uniform(q.len)};
 }
 
+// First key that a row at position pos sees.  A row before the first token counts as the first one, so that no window, however
+// long, takes the difference below -2^31.
+__host__ __device__ __forceinline__ int paged_from(int pos, int window) {
+  const int from = (pos < 0 ? 0 : pos) - window + 1;
+  return window == 0 || from < 0 ? 0 : from;
+}
+
 // Key tiles of one tile of query rows: [first, first + units)
 template <int TR, int KT>
-__device__ __forceinline__ void paged_span(const PagedArgs& a, const PagedSeq& q, int tile, int& first, int& units) {
-  const int x1 = min(q.rows * a.rep, (tile + 1) * TR);
+__host__ __device__ __forceinline__ void paged_span(const PagedArgs& a, const PagedSeq& q, int tile, int& first, int& units) {
+  const int rows = q.rows * a.rep, end = (tile + 1) * TR, x1 = rows < end ? rows : end;
   const int last = q.len - q.rows + (int)div_by(x1 - 1, a.by_rep);
   const int from = q.len - q.rows + (int)div_by(tile * TR, a.by_rep);
-  first = a.window ? max(0, from - a.window + 1) / KT : 0;
+  first = paged_from(from, a.window) / KT;
   units = last < 0 ? 1 : last / KT + 1 - first;
   if (last < 0) first = 0;
 }
 template <int TR>
-__device__ __forceinline__ int paged_tiles(const PagedArgs& a, const PagedSeq& q) {
+__host__ __device__ __forceinline__ int paged_tiles(const PagedArgs& a, const PagedSeq& q) {
   return (q.rows * a.rep + TR - 1) / TR;
 }
 

@@ -142,7 +142,7 @@ __global__ void __launch_bounds__(256, ND <= 8 ? 2 : 1) k_paged_generic(PagedArg
       const int token = valid ? (int)div_by(x, a.by_rep) : 0;
       const int head = p.head * a.rep + (valid ? x - token * a.rep : 0);
       pos[b] = valid ? q.len - q.rows + token : -1;
-      lo[b] = a.window ? max(0, pos[b] - a.window + 1) : 0;
+      lo[b] = paged_from(pos[b], a.window);
       const int64_t q_at = (int64_t)(q.row0 + token) * a.q_stride + (int64_t)head * dh;
       // (behind the head's width: zeros, read from a place that may be read)
       if (a.dtype == KEEP_F32) {
@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(256, ND <= 8 ? 2 : 1) k_paged_generic(PagedArg
     {
       const int x1 = min(q.rows * a.rep, (p.tile + 1) * TR) - 1;
       min_pos = q.len - q.rows + (int)div_by(p.tile * TR, a.by_rep);
-      max_lo = a.window ? max(0, q.len - q.rows + (int)div_by(x1, a.by_rep) - a.window + 1) : 0;
+      max_lo = paged_from(q.len - q.rows + (int)div_by(x1, a.by_rep), a.window);
     }
     // One key tile; MASKED: some row does not see some key of it
     const auto tile = [&](int kt, auto masked_type) __attribute__((always_inline)) {

@@ -156,7 +156,7 @@ __global__ void __launch_bounds__(256, (Few<DH, FMT, RB>::LDS > 80 * 1024 ? 1 : 
       const bool valid = x < q.rows * a.rep;
       const int token = valid ? (int)div_by(x, a.by_rep) : 0;
       pos[b] = valid ? q.len - q.rows + token : -1;
-      lo[b] = a.window ? max(0, pos[b] - a.window + 1) : 0;
+      lo[b] = paged_from(pos[b], a.window);
       const __bf16* qp = static_cast<const __bf16*>(a.q) + (int64_t)(q.row0 + token) * a.q_stride +
                          (int64_t)(p.head * a.rep + (valid ? x - token * a.rep : 0)) * DH;
 #pragma unroll
@@ -168,7 +168,7 @@ __global__ void __launch_bounds__(256, (Few<DH, FMT, RB>::LDS > 80 * 1024 ? 1 : 
       const int x1 = min(q.rows * a.rep, (p.tile + 1) * TR) - 1;
       max_pos = q.len - q.rows + (int)div_by(x1, a.by_rep);
       min_pos = q.len - q.rows + (int)div_by(p.tile * TR, a.by_rep);
-      max_lo = a.window ? max(0, max_pos - a.window + 1) : 0;
+      max_lo = paged_from(max_pos, a.window);
     }
     f32x4 acc[RB][DT];
     float m[RB], l[RB];
@@ -497,12 +497,12 @@ __global__ void __launch_bounds__(256, 2) k_paged_many(PagedArgs a) {
     // the wave's last key and first one, and the keys that every row of the tile sees (lanes without a row are not stored)
     int max_pos = -1, min_lo = 0;
     const int min_pos = q.len - q.rows + (int)div_by(p.tile * TR, a.by_rep);
-    const int max_lo = a.window ? max(0, q.len - q.rows + (int)div_by(min(rows, (p.tile + 1) * TR) - 1, a.by_rep) - a.window + 1) : 0;
+    const int max_lo = paged_from(q.len - q.rows + (int)div_by(min(rows, (p.tile + 1) * TR) - 1, a.by_rep), a.window);
     {
       const int x0 = p.tile * TR + wave * 32, x1 = min(rows, x0 + 32) - 1;
       if (x0 < rows) {
         max_pos = q.len - q.rows + (int)div_by(x1, a.by_rep);
-        min_lo = a.window ? max(0, q.len - q.rows + (int)div_by(x0, a.by_rep) - a.window + 1) : 0;
+        min_lo = paged_from(q.len - q.rows + (int)div_by(x0, a.by_rep), a.window);
       }
     }
     bf16x8 qf[KS];
@@ -511,7 +511,7 @@ __global__ void __launch_bounds__(256, 2) k_paged_many(PagedArgs a) {
       const bool valid = x < rows;
       const int token = valid ? (int)div_by(x, a.by_rep) : 0, head = p.head * a.rep + (valid ? x - token * a.rep : 0);
       pos = valid ? q.len - q.rows + token : -1;
-      lo = a.window ? max(0, pos - a.window + 1) : 0;
+      lo = paged_from(pos, a.window);
       const __bf16* qp = static_cast<const __bf16*>(a.q) + (int64_t)(q.row0 + token) * a.q_stride + (int64_t)head * DH + g * 8;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {

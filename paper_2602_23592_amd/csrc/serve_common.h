@@ -57,6 +57,6 @@ inline FastDiv fast_div(uint32_t d) {
   while ((1ull << l) < d) ++l;
   return FastDiv{(1ull << (31 + l)) / d + 1, 31 + l, d};
 }
-__device__ __forceinline__ uint32_t div_by(uint32_t n, FastDiv f) { return (uint32_t)((uint64_t)n * f.mul >> f.shift); }
+__host__ __device__ __forceinline__ uint32_t div_by(uint32_t n, FastDiv f) { return (uint32_t)((uint64_t)n * f.mul >> f.shift); }
 
 }  // namespace keep
