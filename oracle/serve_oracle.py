@@ -94,8 +94,9 @@ def paged_attention(q, k_pages, v_pages, q_start, kv_len, table, window=0, scale
                 continue
             for h in range(hq):
                 x = (k[lo:pos + 1, h // rep] @ np.float64(q[r, h])) * scale
-                lse[r, h] = x.max() + math.log(np.exp(x - x.max()).sum())
-                p = np.exp(x - lse[r, h])
+                p = np.exp(x - x.max())                # (a difference from lse would lose log(sum) beside scores of 2^50)
+                lse[r, h] = x.max() + math.log(p.sum())
+                p /= p.sum()
                 out[r, h] = p @ v[lo:pos + 1, h // rep]
                 absum[r, h] = p @ np.abs(v[lo:pos + 1, h // rep])
     return out, lse, absum

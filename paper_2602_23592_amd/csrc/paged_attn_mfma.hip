@@ -691,13 +691,26 @@ __global__ void __launch_bounds__(256, 2) k_paged_many(PagedArgs a) {
               for (int e = 0; e < 16; ++e) acc[nt][e] *= alpha;
             m = m_new;
           }
+          // fma(s, factor, -ref) keeps s factor exact, so the rounding of ref multiplies all of a row's weights alike and leaves
+          // their quotients; from 2^31 on it would be all there is of them (2^128, or nothing).  Rows whose maximum lies beyond
+          // FAR, where it could reach 2, round the products first, as it was.
+          constexpr float FAR = 16777216.f;
+          float by = factor;
+          if (F::WIDE && __ballot(fabsf(ref) > FAR)) {
+            const bool far = fabsf(ref) > FAR;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+              for (int e = 0; e < 16; ++e) s[h][e] = far ? s[h][e] * factor : s[h][e];
+            by = far ? 1.f : factor;
+          }
           uint32_t pk[2][8];
 #pragma unroll
           for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int e = 0; e < 16; e += 2) {
-              float p0 = __builtin_amdgcn_exp2f(F::WIDE ? __builtin_fmaf(s[h][e], factor, -ref) : s[h][e] - ref);
-              float p1 = __builtin_amdgcn_exp2f(F::WIDE ? __builtin_fmaf(s[h][e + 1], factor, -ref) : s[h][e + 1] - ref);
+              float p0 = __builtin_amdgcn_exp2f(F::WIDE ? __builtin_fmaf(s[h][e], by, -ref) : s[h][e] - ref);
+              float p1 = __builtin_amdgcn_exp2f(F::WIDE ? __builtin_fmaf(s[h][e + 1], by, -ref) : s[h][e + 1] - ref);
               l += p0 + p1;
               if constexpr (!F::WIDE) {
                 const float* v = ksc + KT + h * 32 + 8 * (e >> 2) + 4 * g + (e & 3);

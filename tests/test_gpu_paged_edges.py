@@ -1,7 +1,9 @@
 """keep_paged_attention at the ends of its arguments' ranges, against the 64-bit oracle."""
+import numpy as np
 import pytest
 import torch
 
+from oracle import serve_oracle as so
 from test_gpu_paged_attention import FORMATS, RAGGED, Batch
 
 pytestmark = pytest.mark.gpu
@@ -18,3 +20,41 @@ def test_windows_that_hide_nothing(dtype, fmt, dh, extra):
     for window in (capacity - 1, capacity, 2 ** 31 - 1025, 2 ** 31 - 1):
         got = b.check(window=window)
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def check_signs(b, power, scale):
+    g = torch.Generator().manual_seed(power)
+    sign = lambda t: (torch.randint(0, 2, t.shape, generator=g) * 2 - 1).float().cuda()
+    b.q.copy_(sign(b.q))
+    if b.cache.k_scale is None:
+        b.cache.k.copy_(sign(b.cache.k) * 2.0 ** power)
+    else:
+        b.cache.k.copy_(sign(b.cache.k).to(b.cache.k.dtype))
+        b.cache.k_scale.fill_(2.0 ** power)
+    out, lse = b.run(scale=scale)
+    k, v = b.numbers()
+    dh, end = b.q.shape[2], int(b.start[-1])
+    want, wl, absum = (t[:end] for t in so.paged_attention(b.q.double().cpu().numpy(), k, v, b.start, b.total,
+                                                           b.table.cpu().numpy(), 0, scale))
+    # From 2^14 on a row's scores lie 4096 or more apart or are equal: the largest share the row, with equal weights.  Below, a
+    # score is off by 2^-24 of its size three times (log2(e), its product with the scale, the product with the score), a
+    # probability by twice that (its own and the norm's).  Then the rounded probability, the sum, the result; of the log-sum-exp
+    # three roundings of the largest score's place, the sum with the logarithm, and two of ln 2.
+    err = 3 * 2.0 ** -24 * dh * 2.0 ** power * 0.125 if power < 14 else 0.0
+    half = torch.finfo(b.dtype).eps / 2
+    o, l = out.double().cpu().numpy()[:end], lse.double().cpu().numpy()[:end]
+    assert np.isfinite(o).all() and np.isfinite(l).all(), b.new
+    assert (np.abs(o - want) <= (2 * err + 2.0 ** -8 + 2.0 ** -13) * absum + half * np.abs(want)).all(), b.new
+    assert (np.abs(l - wl) <= 6 * 2.0 ** -24 * np.abs(wl) + err + 2.0 ** -13).all(), b.new
+
+
+@pytest.mark.parametrize("dtype,fmt,dh", [("f32", "f32", 64), ("f32", "fp8", 80), ("bf16", "bf16", 64), ("bf16", "bf16", 128),
+                                          ("bf16", "fp8", 128), ("bf16", "int8", 64), ("bf16", "bf16", 256)])
+@pytest.mark.parametrize("power", [3, 14, 17, 18, 19, 21, 26, 31, 36, 60, 100, 116])
+@pytest.mark.parametrize("scale", [0.125, -0.125])
+def test_scores_of_any_finite_size(dtype, fmt, dh, power, scale):
+    """Queries of ones and keys of 2^power, signs at random: scores are whole multiples of 2^power, so binary32 sums them exactly,
+    tells different ones apart and keeps equal ones equal, and the largest of a row share it, however large they are.  Chunks
+    (tiles of 128, 32 and 16 query rows) and single tokens."""
+    for seqs in ([(70, 300), (200, 333), (1, 77), (3, 500)], [(12, 300), (12, 90)], [(7, 300), (1, 40)]):
+        check_signs(Batch(seqs, 4, 2, dh, FORMATS[dtype], fmt, 16, seed=power), power, scale)
