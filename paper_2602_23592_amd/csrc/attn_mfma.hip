@@ -42,7 +42,7 @@ __device__ __forceinline__ bf16x8 cat4(s16x4 a, s16x4 b) {
   return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-constexpr float M_FLOOR = -1.0e30f;  // running max starts here (finite, so a fully masked tile gives alpha = 1, p = 0)
+constexpr float M_FLOOR = -3.0e38f;  // running max starts here (finite, so a fully masked tile gives alpha = 1, p = 0)
 constexpr int PART_FLOATS = 128 * DH;  // partial O of one (item, KV head): [dh/4][q 128][4]
 
 __global__ void __launch_bounds__(256, 2)
@@ -209,14 +209,26 @@ __global__ void __launch_bounds__(256, 2)
           for (int e = 0; e < 16; ++e) oacc[nt][e] *= alpha;
         m_run = m_new;
       }
+      // The fma keeps the product exact, so the rounding of m_new multiplies all of a row's weights alike; from 2^31 on that
+      // would be 2^128 or nothing.  Rows with a maximum beyond FAR, where the rounding could reach 2, round the products first.
+      constexpr float FAR = 16777216.f;
+      const bool far = fabsf(m_new) > FAR && m_new != M_FLOOR;
+      float factor = scale_log2e;
+      if (__builtin_amdgcn_ballot_w64(far) != 0) {
+#pragma unroll
+        for (int st = 0; st < 2; ++st)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sacc[st][e] = far ? sacc[st][e] * scale_log2e : sacc[st][e];
+        factor = far ? 1.f : scale_log2e;
+      }
       float psum = 0.f;
       uint32_t pk[2][8];
 #pragma unroll
       for (int st = 0; st < 2; ++st)
 #pragma unroll
         for (int e = 0; e < 16; e += 2) {
-          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[st][e], scale_log2e, -m_new));
-          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[st][e + 1], scale_log2e, -m_new));
+          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[st][e], factor, -m_new));
+          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[st][e + 1], factor, -m_new));
           psum += p0 + p1;
           pk[st][e >> 1] = pack_bf16x2(p0, p1);
         }
