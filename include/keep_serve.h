@@ -71,7 +71,8 @@ typedef struct {
 
 /* Turns the queries and keys of n_rows tokens.
  *   q_in, k_in -> q_out, k_out: DEVICE, any element-aligned address; out may be the in pointer itself (with the same stride),
- *     otherwise the two must not overlap.  The pointers of q (of k) are not read when n_q_heads (n_kv_heads) is 0.
+ *     otherwise the two must not share an element (other columns of the same rows, with the same stride, are separate).  The
+ *     pointers of q (of k) are not read when n_q_heads (n_kv_heads) is 0.
  *   positions: DEVICE int32 [n_rows], any value; a negative one turns back.
  *   freq: DEVICE double [rot_dim / 2].
  * Angles are formed and reduced in double, products in binary32, results rounded once.
@@ -137,7 +138,8 @@ typedef struct {
  * n_seqs sequences; 0 if a description is invalid. */
 uint64_t keep_paged_attention_workspace_bytes(const keep_paged_cache* cache, int32_t n_q_heads, int32_t n_seqs);
 
-/*   q, out: DEVICE, 16-byte aligned, [n_rows] rows of [n_q_heads][head_dim]; they must not overlap.
+/*   q, out: DEVICE, 16-byte aligned, [n_rows] rows of [n_q_heads][head_dim]; they must not share an element (other columns of
+ *     the same rows, with the same stride, are separate).
  *   q_start: DEVICE int32 [n_seqs + 1], not decreasing, within [0, n_rows] (clamped to that).
  *   kv_len: DEVICE int32 [n_seqs] (clamped to [0, max_pages * page_size]).
  *   page_table: DEVICE int32 [n_seqs, max_pages]; entries behind a sequence's last page are not read, others are

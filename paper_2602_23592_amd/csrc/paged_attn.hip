@@ -505,7 +505,7 @@ extern "C" keep_status keep_paged_attention(const keep_paged_attention_desc* d, 
     return serve_fail(KEEP_ERR_INVALID_ARG, "%s: q / q_start / kv_len / page_table / out / workspace is NULL", me);
   if (!aligned16(q) || !aligned16(out) || reinterpret_cast<uintptr_t>(workspace) % 256)
     return serve_fail(KEEP_ERR_INVALID_ARG, "%s: q, out or workspace is not aligned", me);
-  if (overlaps(q, row_span(d->n_rows, d->q_stride, width, size), out, row_span(d->n_rows, d->out_stride, width, size)))
+  if (overlaps({q, d->q_stride, width}, {out, d->out_stride, width}, d->n_rows, size))
     return serve_fail(KEEP_ERR_INVALID_ARG, "%s: q and out overlap", me);
   if (workspace_bytes < keep_paged_attention_workspace_bytes(cache, d->n_q_heads, d->n_seqs))
     return serve_fail(KEEP_ERR_WORKSPACE, "%s: workspace of %llu bytes is too small", me, (unsigned long long)workspace_bytes);

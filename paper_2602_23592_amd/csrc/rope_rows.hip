@@ -197,7 +197,7 @@ extern "C" keep_status keep_rope_rows(const keep_rope_rows_desc* d, const void* 
     if (reinterpret_cast<uintptr_t>(p.in) % size || reinterpret_cast<uintptr_t>(p.out) % size)
       return serve_fail(KEEP_ERR_INVALID_ARG, "%s: a pointer is not aligned to its elements", me);
     if (p.in != p.out || p.is != p.os) {
-      if (overlaps(p.in, row_span(d->n_rows, p.is, p.w, size), p.out, row_span(d->n_rows, p.os, p.w, size)))
+      if (overlaps({p.in, p.is, p.w}, {p.out, p.os, p.w}, d->n_rows, size))
         return serve_fail(KEEP_ERR_INVALID_ARG, "%s: input and output overlap without being the same rows", me);
       copy_rest = true;
     }

@@ -31,15 +31,24 @@ inline int dtype_size(int32_t t) { return t == KEEP_F32 ? 4 : 2; }
 inline int format_size(int32_t f) { return f == KEEP_CACHE_F32 ? 4 : f == KEEP_CACHE_BF16 ? 2 : 1; }
 inline bool format_scaled(int32_t f) { return f == KEEP_CACHE_FP8 || f == KEEP_CACHE_INT8; }
 
-// bytes [a, a + na) and [b, b + nb) share an address
-inline bool overlaps(const void* a, uint64_t na, const void* b, uint64_t nb) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return na && nb && x < y + nb && y < x + na;
-}
+// n_rows rows of `width` elements, `stride` elements apart
+struct Rows {
+  const void* at;
+  int64_t stride, width;
+};
 
-// bytes from the first row to the end of the last one
-inline uint64_t row_span(int64_t n_rows, int64_t stride, int64_t width, int size) {
-  return n_rows > 0 ? ((uint64_t)(n_rows - 1) * (uint64_t)stride + (uint64_t)width) * (uint64_t)size : 0;
+// Whether two sets of rows share an element.  With equal strides both repeat at the stride's distance, and slices of the same wide
+// rows lie beside each other though the first and last address of one enclose the other; with unequal ones that counts as
+// overlapping.
+inline bool overlaps(const Rows& a, const Rows& b, int64_t n_rows, int size) {
+  if (n_rows < 1 || a.width < 1 || b.width < 1) return false;
+  const uint64_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
+  const auto span = [&](const Rows& r) { return ((uint64_t)(n_rows - 1) * (uint64_t)r.stride + (uint64_t)r.width) * (uint64_t)size; };
+  if (x >= y + span(b) || y >= x + span(a)) return false;
+  if (n_rows == 1 || a.stride != b.stride) return true;
+  const uint64_t step = (uint64_t)a.stride * (uint64_t)size;
+  const uint64_t off = y >= x ? (y - x) % step : step - 1 - (x - y - 1) % step;  // of b's rows behind a's
+  return off < (uint64_t)a.width * size || off + (uint64_t)b.width * size > step;
 }
 
 // paged_cache.hip: KEEP_OK, or the status with its text set

@@ -153,3 +153,12 @@ def test_sample_refuses(kw, status):
 
 def test_decode_sampled_needs_a_context():
     assert kb.load_library().keep_decode_sampled(None, P, P, P, P, P, 1, 1, 1, None, None, None, None, None) == ARG
+
+
+@pytest.mark.parametrize("off", [0, 4, 252, -4, -252, 512 * 3 + 200, 260, 512 * 2 - 100])
+def test_slices_of_the_same_rows_that_share_an_element(off):
+    """rows of 256 values, 512 apart, each 4 bytes: an output that begins `off` values behind the input"""
+    far = P + (1 << 22)
+    if off:
+        assert _rope(q_in_stride=512, q_out_stride=512, q=far, q_out=far + 4 * off) == ARG and "overlap" in text()
+    assert _attend(q_stride=512, out_stride=512, q=far, out=far + 4 * off) == ARG and "overlap" in text()
