@@ -71,8 +71,9 @@ typedef struct {
 
 /* Turns the queries and keys of n_rows tokens.
  *   q_in, k_in -> q_out, k_out: DEVICE, any element-aligned address; out may be the in pointer itself (with the same stride),
- *     otherwise the two must not share an element (other columns of the same rows, with the same stride, are separate).  The
- *     pointers of q (of k) are not read when n_q_heads (n_kv_heads) is 0.
+ *     otherwise the two must not share an element (other columns of the same rows, with the same stride, are separate).  q_out
+ *     must share none with k_in or k_out, nor q_in with k_out.  The pointers of q (of k) are not read when n_q_heads
+ *     (n_kv_heads) is 0.
  *   positions: DEVICE int32 [n_rows], any value; a negative one turns back.
  *   freq: DEVICE double [rot_dim / 2].
  * Angles are formed and reduced in double, products in binary32, results rounded once.

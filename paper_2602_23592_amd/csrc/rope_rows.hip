@@ -204,6 +204,10 @@ extern "C" keep_status keep_rope_rows(const keep_rope_rows_desc* d, const void* 
     vec = vec && aligned16(p.in) && aligned16(p.out) && p.is * size % 16 == 0 && p.os * size % 16 == 0;
   }
   if (d->n_rows == 0) return KEEP_OK;
+  // queries beside keys: rows that one of them writes belong to it alone
+  const Rows qi{q_in, d->q_in_stride, qw}, qo{q_out, d->q_out_stride, qw}, ki{k_in, d->k_in_stride, kw}, ko{k_out, d->k_out_stride, kw};
+  if (overlaps(qo, ki, d->n_rows, size) || overlaps(qo, ko, d->n_rows, size) || overlaps(qi, ko, d->n_rows, size))
+    return serve_fail(KEEP_ERR_INVALID_ARG, "%s: rows of queries and of keys overlap", me);
   RopeArgs a{q_in, k_in, q_out, k_out, d->q_in_stride, d->q_out_stride, d->k_in_stride, d->k_out_stride, positions, freq,
              d->n_rows, d->n_q_heads, d->n_q_heads + d->n_kv_heads, d->head_dim, d->rot_dim / 2, 1, d->magnitude, copy_rest};
   // one row per workgroup while rows are fewer than the chip holds workgroups, then four: the table's 64 pairs of a

@@ -162,3 +162,12 @@ def test_slices_of_the_same_rows_that_share_an_element(off):
     if off:
         assert _rope(q_in_stride=512, q_out_stride=512, q=far, q_out=far + 4 * off) == ARG and "overlap" in text()
     assert _attend(q_stride=512, out_stride=512, q=far, out=far + 4 * off) == ARG and "overlap" in text()
+
+
+@pytest.mark.parametrize("kw", [
+    dict(k=P), dict(k_out=P), dict(k=P, k_out=P), dict(q_out=P + 4096 * 4), dict(k_out=P + 512),                # separate rows
+    dict(q_in_stride=512, q_out_stride=512, k_in_stride=512, k_out_stride=512, k=P + 1020, k_out=P + 1020),   # slices of fused rows
+    dict(q_in_stride=512, q_out_stride=512, k_in_stride=512, k_out_stride=512, k=P + 1024, k_out=P + 2040),
+    dict(n_rows=1, k=P + 1020, k_out=P + 1020)])
+def test_rope_refuses_queries_and_keys_that_share_an_element(kw):
+    assert _rope(**kw) == ARG and "overlap" in text()
