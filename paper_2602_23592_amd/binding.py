@@ -251,6 +251,15 @@ def _stream_handle(s) -> Optional[int]:
     return s.cuda_stream if hasattr(s, "cuda_stream") else int(s)
 
 
+def _forced_tokens(tokens: Optional[Sequence[int]], n_new: int):
+    """(array that owns the memory, its address) of the tokens to feed: the library reads n_new - 1 of them"""
+    if tokens is None:
+        return None, None
+    if len(tokens) < n_new - 1:
+        raise KeepError(KEEP_ERR_INVALID_ARG, "forced_tokens has %d entries, %d new tokens need %d" % (len(tokens), n_new, n_new - 1))
+    return _i32_array(list(tokens) if len(tokens) else [0])
+
+
 class KeepPrompt:
     """Keeps the host arrays of a keep_prompt alive and exposes the C struct."""
 
@@ -722,9 +731,7 @@ class KeepContext:
                forced_tokens: Optional[Sequence[int]] = None):
         """Greedy tokens after a prompt of n_ctx tokens; caches are [n_layers, cache_rows, Hkv, dh]."""
         out = np.zeros(max(1, n_new), dtype=np.int32)
-        fp = None
-        if forced_tokens is not None:
-            f, fp = _i32_array(list(forced_tokens) if len(forced_tokens) else [0])
+        f, fp = _forced_tokens(forced_tokens, n_new)
         self._check(self.lib.keep_decode(self.handle, final_norm.data_ptr(), lm_head.data_ptr(), x_last.data_ptr(),
                                          k_cache.data_ptr(), v_cache.data_ptr(), k_cache.shape[1], n_ctx, n_new,
                                          out.ctypes.data_as(C.POINTER(C.c_int32)), _ptr(logits_out), fp))
@@ -738,9 +745,7 @@ class KeepContext:
         u = np.ascontiguousarray(np.asarray(uniform, dtype=np.float32))
         n_new = len(u)
         out, probs = np.zeros(max(1, n_new), dtype=np.int32), np.zeros(max(1, n_new), dtype=np.float32)
-        fp = None
-        if forced_tokens is not None:
-            f, fp = _i32_array(list(forced_tokens) if len(forced_tokens) else [0])
+        f, fp = _forced_tokens(forced_tokens, n_new)
         how = Sampling(temperature, top_k, top_p, min_p, u.ctypes.data_as(C.POINTER(C.c_float)))
         self._check(self.lib.keep_decode_sampled(
             self.handle, final_norm.data_ptr(), lm_head.data_ptr(), x_last.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),

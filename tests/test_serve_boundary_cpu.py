@@ -4,6 +4,7 @@ import math
 
 import numpy as np
 import pytest
+import torch
 
 from oracle import serve_oracle as so
 from paper_2602_23592_amd import binding as kb
@@ -171,3 +172,32 @@ def test_slices_of_the_same_rows_that_share_an_element(off):
     dict(n_rows=1, k=P + 1020, k_out=P + 1020)])
 def test_rope_refuses_queries_and_keys_that_share_an_element(kw):
     assert _rope(**kw) == ARG and "overlap" in text()
+
+
+class _NoCall:
+    """A library that answers every call, and counts them"""
+    calls = 0
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls += 1
+            return kb.KEEP_OK
+        return call
+
+
+@pytest.mark.parametrize("n_new,forced,ok", [(3, [], False), (3, [5], False), (64, [1] * 62, False), (1, [], True), (3, [5, 6], True),
+                                             (3, [5, 6, 7], True), (3, None, True)])
+def test_forced_tokens_shorter_than_what_the_library_reads_are_refused(n_new, forced, ok):
+    t = torch.zeros(2, 4)
+    for sampled in (False, True):
+        ctx = object.__new__(kb.KeepContext)
+        ctx.lib, ctx.handle = _NoCall(), None
+        call = (lambda: ctx.decode_sampled(t, t, t, t, t, 1, [0.5] * n_new, forced_tokens=forced)) if sampled else \
+            (lambda: ctx.decode(t, t, t, t, t, 1, n_new, forced_tokens=forced))
+        if ok:
+            call()
+            assert ctx.lib.calls == 1
+        else:
+            with pytest.raises(kb.KeepError, match="forced_tokens"):
+                call()
+            assert ctx.lib.calls == 0
