@@ -335,6 +335,8 @@ def select_groups_static(S: torch.Tensor, groups: torch.Tensor, group_len: torch
 
 
 # ---- the operators of include/keep_serve.h ------------------------------------------------------------------
+# `stream` of these calls: a torch stream or a hipStream_t, by default the current stream of the tensors' device.  That the
+# tensors' contents are there when the stream reaches the call is the caller's; their memory may be dropped behind the call.
 _DTYPES = {torch.float32: KEEP_F32, torch.bfloat16: KEEP_BF16}
 _FORMATS = {torch.float32: KEEP_CACHE_F32, torch.bfloat16: KEEP_CACHE_BF16, torch.float8_e4m3fn: KEEP_CACHE_FP8,
             torch.int8: KEEP_CACHE_INT8}
@@ -357,15 +359,30 @@ def _launch(device: torch.device, stream, call, *args):
         raise KeepError(st, _lib.keep_last_error(None).decode())
 
 
+def _stream_object(stream, device: torch.device) -> torch.cuda.Stream:
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    handle = _stream_handle(stream)
+    return torch.cuda.ExternalStream(handle, device=device) if handle else torch.cuda.default_stream(device)
+
+
 def _empty(shape, dtype: torch.dtype, device: torch.device, stream) -> torch.Tensor:
     """New memory that belongs to the stream of the call: its next use there waits for the call, wherever the tensor is dropped"""
     if stream is None:
         return torch.empty(shape, dtype=dtype, device=device)
-    if not isinstance(stream, torch.cuda.Stream):
-        handle = _stream_handle(stream)
-        stream = torch.cuda.ExternalStream(handle, device=device) if handle else torch.cuda.default_stream(device)
-    with torch.cuda.stream(stream):
+    with torch.cuda.stream(_stream_object(stream, device)):
         return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _hold(device: torch.device, stream, *tensors: Optional[torch.Tensor]):
+    """Memory of a call's tensors is not handed out again before the call is done, also where they are dropped behind it and
+    belong to another stream than its own"""
+    if stream is None or (_stream_handle(stream) or 0) == torch.cuda.current_stream(device).cuda_stream:
+        return
+    on = _stream_object(stream, device)
+    for t in tensors:
+        if t is not None and t.is_cuda:
+            t.record_stream(on)
 
 
 def _array(name: str, t: Optional[torch.Tensor], dtype, numel: int, device: torch.device, optional: bool = False):
@@ -427,6 +444,7 @@ def rope_rows(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: t
         if k_out.shape != k.shape or rows != n or dk != d:
             _refuse("rows or head_dim of keys differ from the queries', or k_out from k")
     pairs = freq.numel()
+    _hold(device, stream, q, k, q_out, k_out, positions, freq)
     desc = RopeRowsDesc(_DTYPES[dtype], n, hq, hkv, d, 2 * pairs, layout, magnitude, qi, qo, ki, ko)
     _launch(device, stream, lib.keep_rope_rows, C.byref(desc), _ptr(q), _ptr(q_out), _ptr(k), _ptr(k_out),
             _array("positions", positions, torch.int32, n, device), _array("freq", freq, torch.float64, pairs, device))
@@ -471,6 +489,7 @@ class PagedCache:
         n, h, d = k.shape
         if _heads("v", v, self.device, k.dtype) != stride or v.shape != k.shape or h != self.c.n_kv_heads or d != self.c.head_dim:
             _refuse("k and v must be alike, [rows, n_kv_heads, head_dim]")
+        _hold(self.device, stream, k, v, slots, self.k, self.v, self.k_scale, self.v_scale)
         _launch(self.device, stream, call, C.byref(self.c), _DTYPES[k.dtype], k.data_ptr(), v.data_ptr(), n, stride,
                 _array("slots", slots, torch.int32, n, self.device))
 
@@ -509,6 +528,7 @@ def paged_attention(q: torch.Tensor, cache: PagedCache, q_start: torch.Tensor, k
     desc = PagedAttentionDesc(_DTYPES[q.dtype], seqs, n, hq, page_table.shape[1], window, scale, stride,
                               _heads("out", out, q.device, q.dtype))
     dev = cache.device
+    _hold(dev, stream, q, q_start, kv_len, page_table, out, lse, workspace, cache.k, cache.v, cache.k_scale, cache.v_scale)
     _launch(dev, stream, cache.lib.keep_paged_attention, C.byref(desc), C.byref(cache.c), q.data_ptr(),
             _array("q_start", q_start, torch.int32, seqs + 1, dev), _array("kv_len", kv_len, torch.int32, seqs, dev),
             _array("page_table", page_table, torch.int32, page_table.numel(), dev), out.data_ptr(),
@@ -535,6 +555,7 @@ def sample(logits: torch.Tensor, uniform: torch.Tensor, temperature: Optional[to
         tokens = _empty(n, torch.int32, dev, stream)
     if workspace is None:
         workspace = _empty(max(1, sample_workspace_bytes(n, vocab)), torch.uint8, dev, stream)
+    _hold(dev, stream, logits, uniform, temperature, top_k, top_p, min_p, tokens, probs, workspace)
     desc = SampleDesc(_DTYPES[logits.dtype], n, vocab, logits.stride(0) if n > 1 else vocab)
     _launch(dev, stream, lib.keep_sample, C.byref(desc), logits.data_ptr(), _array("uniform", uniform, torch.float32, n, dev),
             _array("temperature", temperature, torch.float32, n, dev, True), _array("top_k", top_k, torch.int32, n, dev, True),
