@@ -346,6 +346,11 @@ def _refuse(text: str):
     raise KeepError(KEEP_ERR_INVALID_ARG, text)
 
 
+def _on_gpu(device: torch.device):
+    if device.type != "cuda":
+        _refuse("tensors must be on the GPU, these are on %s" % device)
+
+
 def _launch(device: torch.device, stream, call, *args):
     """One call on `stream`, by default the current one of the tensors' device, with that device current."""
     if stream is None:
@@ -428,6 +433,7 @@ def rope_rows(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: t
     if ref is None:
         _refuse("neither queries nor keys")
     device, dtype = ref.device, ref.dtype
+    _on_gpu(device)
     if dtype not in _DTYPES or ref.dim() != 3 or (q is None and q_out is not None) or (k is None and k_out is not None):
         _refuse("queries and keys must be [rows, heads, head_dim] in float32 or bfloat16, outputs go with inputs")
     n, _, d = ref.shape
@@ -551,6 +557,7 @@ def sample(logits: torch.Tensor, uniform: torch.Tensor, temperature: Optional[to
         _refuse("logits must be [rows, vocab] in float32 or bfloat16 with adjacent values")
     n, vocab = logits.shape
     dev = logits.device
+    _on_gpu(dev)
     if tokens is None:
         tokens = _empty(n, torch.int32, dev, stream)
     if workspace is None:

@@ -201,3 +201,13 @@ def test_forced_tokens_shorter_than_what_the_library_reads_are_refused(n_new, fo
             with pytest.raises(kb.KeepError, match="forced_tokens"):
                 call()
             assert ctx.lib.calls == 0
+
+
+@pytest.mark.parametrize("stream", [None, 0, 64])
+def test_tensors_on_the_host_are_refused(stream):
+    """like any other wrong tensor, whatever the stream"""
+    x, pos, freq = torch.zeros(3, 2, 64), torch.zeros(3, dtype=torch.int32), torch.ones(32, dtype=torch.float64)
+    for call in (lambda: kb.rope_rows(x, None, pos, freq, stream=stream), lambda: kb.sample(x[:, 0], x[:, 0, 0].clone(), stream=stream),
+                 lambda: kb.PagedCache(x[None], x[None].clone())):
+        with pytest.raises(kb.KeepError):
+            call()
