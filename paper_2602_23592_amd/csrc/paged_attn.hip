@@ -437,14 +437,16 @@ constexpr bool paged_wide_tiles(int format, int head_dim) { return head_dim <= (
 template <int FORMAT>
 static void launch_generic(const PagedArgs& a, int rows, hipStream_t s) {
   const int dh = a.c.head_dim;
-  if (rows == 16)
-    return dh <= 64    ? launch_generic<FORMAT, 4, 1>(a, s)
-           : dh <= 80  ? launch_generic<FORMAT, 5, 1>(a, s)
-           : dh <= 128 ? launch_generic<FORMAT, 8, 1>(a, s)
-                       : launch_generic<FORMAT, 16, 1>(a, s);
-  if (dh <= 64) return launch_generic<FORMAT, 4, 2>(a, s);
-  if (dh <= 80) return launch_generic<FORMAT, 5, 2>(a, s);
-  if constexpr (paged_wide_tiles(FORMAT, 128)) launch_generic<FORMAT, 8, 2>(a, s);
+  // (tiles of 16 rows where there are none of 32: they and their join fit a workspace laid out for 32)
+  if (rows == 32 && paged_wide_tiles(FORMAT, dh)) {
+    if (dh <= 64) return launch_generic<FORMAT, 4, 2>(a, s);
+    if (dh <= 80) return launch_generic<FORMAT, 5, 2>(a, s);
+    if constexpr (paged_wide_tiles(FORMAT, 128)) return launch_generic<FORMAT, 8, 2>(a, s);
+  }
+  return dh <= 64    ? launch_generic<FORMAT, 4, 1>(a, s)
+         : dh <= 80  ? launch_generic<FORMAT, 5, 1>(a, s)
+         : dh <= 128 ? launch_generic<FORMAT, 8, 1>(a, s)
+                     : launch_generic<FORMAT, 16, 1>(a, s);
 }
 
 void launch_paged_generic(const PagedArgs& a, int rows, hipStream_t s) {
