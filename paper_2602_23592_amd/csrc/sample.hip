@@ -350,7 +350,7 @@ struct SampleArgs {
 };
 
 // ---- the steps; every thread of the workgroup takes part in each -------------------------------------------------
-__device__ __forceinline__ Row row_of(const SampleArgs& a, int row, SampleLds& l) {
+__device__ __forceinline__ Row row_of(const SampleArgs& a, int row) {
   Row r{};
   r.x = static_cast<const char*>(a.logits) + (int64_t)row * a.row_stride * (a.dtype == KEEP_F32 ? 4 : 2);
   r.dtype = a.dtype;
@@ -702,7 +702,7 @@ __device__ __forceinline__ void whole_row(const SampleArgs& a, int row, const Ro
 __global__ void __launch_bounds__(ST) k_sample_row(SampleArgs a) {
   __shared__ SampleLds l;
   const int row = blockIdx.x;
-  Row r = row_of(a, row, l);
+  Row r = row_of(a, row);
   const Wishes w = wishes_of(a, row);
   if (!set_scale(a, row, largest(r, 0, r.n, l), true, w, r)) return;
   whole_row(a, row, r, w, w.light, l);
@@ -723,7 +723,7 @@ __device__ __forceinline__ uint64_t best_of(const SampleArgs& a, int row) {
 __global__ void __launch_bounds__(ST) k_sample_max(SampleArgs a) {
   __shared__ SampleLds l;
   const int row = blockIdx.y, begin = blockIdx.x * a.part_len;
-  const Row r = row_of(a, row, l);
+  const Row r = row_of(a, row);
   // (the next step's sums start from zero)
   for (int b = blockIdx.x * ST + threadIdx.x; b < BINS; b += gridDim.x * ST)
     a.mass[(int64_t)row * BINS + b] = 0, a.count[(int64_t)row * BINS + b] = 0;
@@ -735,7 +735,7 @@ __global__ void __launch_bounds__(ST) k_sample_max(SampleArgs a) {
 __global__ void __launch_bounds__(ST) k_sample_bins(SampleArgs a) {
   __shared__ SampleLds l;
   const int row = blockIdx.y, begin = blockIdx.x * a.part_len;
-  Row r = row_of(a, row, l);
+  Row r = row_of(a, row);
   const Wishes w = wishes_of(a, row);
   if (!set_scale(a, row, best_of(a, row), false, w, r)) return;
   clear_bins(l);
@@ -753,7 +753,7 @@ __global__ void __launch_bounds__(ST) k_sample_bins(SampleArgs a) {
 __global__ void __launch_bounds__(ST) k_sample_list(SampleArgs a) {
   __shared__ SampleLds l;
   const int row = blockIdx.y, begin = blockIdx.x * a.part_len;
-  Row r = row_of(a, row, l);
+  Row r = row_of(a, row);
   const Wishes w = wishes_of(a, row);
   if (!set_scale(a, row, best_of(a, row), blockIdx.x == 0, w, r)) return;
   for (int b = threadIdx.x; b < BINS; b += ST) {
