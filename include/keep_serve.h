@@ -148,9 +148,12 @@ uint64_t keep_paged_attention_workspace_bytes(const keep_paged_cache* cache, int
  *   lse: DEVICE float [n_rows, n_q_heads] or NULL: log-sum-exp of each row's scaled scores.
  *   workspace: DEVICE, 256-byte aligned, at least keep_paged_attention_workspace_bytes.
  * Rows of out and lse that no sequence owns are left as they were.  A key or value that is not finite reaches only the
- * rows that see it.  Sums and statistics are binary32 in an order that depends on the lengths alone, so equal calls give
- * equal bits.  bf16 queries with heads of 64, 128 or 256 over a bf16 or 8-bit cache run on the bf16 matrix instruction,
- * with the probabilities rounded to bf16; everything else on the fp32 one.
+ * rows that see it.  Sums and statistics are binary32.  Their order depends on the two descriptions, q_start and kv_len (those
+ * of all sequences: a launch's work is divided among workgroups by them), and in tiles with values that are not finite on
+ * these; it does not depend on page numbers, contents of the workspace or timing.  So equal calls give equal bits, while other
+ * neighbours in the batch, rows for padding or a wider page table can change a row's last bits.
+ * bf16 queries with heads of 64, 128 or 256 over a bf16 or 8-bit cache (of less than 64 GB of keys) run on the bf16 matrix
+ * instruction, with the probabilities rounded to bf16; everything else on the fp32 one.
  * Errors: INVALID_ARG, SHAPE, WORKSPACE (workspace_bytes too small), HIP. */
 keep_status keep_paged_attention(const keep_paged_attention_desc* desc, const keep_paged_cache* cache, const void* q,
                                  const int32_t* q_start, const int32_t* kv_len, const int32_t* page_table, void* out,

@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from oracle import serve_oracle as so
+from paper_2602_23592_amd import binding as kb
 from test_gpu_paged_attention import FORMATS, RAGGED, Batch
 
 pytestmark = pytest.mark.gpu
@@ -58,3 +59,28 @@ def test_scores_of_any_finite_size(dtype, fmt, dh, power, scale):
     (tiles of 128, 32 and 16 query rows) and single tokens."""
     for seqs in ([(70, 300), (200, 333), (1, 77), (3, 500)], [(12, 300), (12, 90)], [(7, 300), (1, 40)]):
         check_signs(Batch(seqs, 4, 2, dh, FORMATS[dtype], fmt, 16, seed=power), power, scale)
+
+
+@pytest.mark.parametrize("dtype,fmt,dh", [("f32", "f32", 64), ("f32", "int8", 128), ("bf16", "bf16", 128), ("bf16", "fp8", 64),
+                                          ("bf16", "bf16", 256)])
+def test_what_the_order_of_sums_depends_on(dtype, fmt, dh):
+    """Other page numbers: the same bits.  A wider table, padding rows, empty sequences: the same results."""
+    b = Batch([(1, 900), (20, 333), (3, 3)], 4, 2, dh, FORMATS[dtype], fmt, 16, seed=2)
+    want = b.check()
+    pages = b.cache.k.shape[0]
+    to = torch.randperm(pages, generator=torch.Generator().manual_seed(9)).cuda()
+    moved = [None if t is None else torch.empty_like(t) for t in (b.cache.k, b.cache.v, b.cache.k_scale, b.cache.v_scale)]
+    for t, m in zip((b.cache.k, b.cache.v, b.cache.k_scale, b.cache.v_scale), moved):
+        if t is not None:
+            (m.view(torch.uint8) if m.element_size() == 1 else m)[to] = t.view(torch.uint8) if t.element_size() == 1 else t
+    old, b.cache, table = b.cache, kb.PagedCache(*moved), b.table
+    b.table = torch.where(table < pages, to[table.clamp(max=pages - 1).long()].int(), table)
+    got = b.run()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    b.cache = old
+    b.table = torch.cat([table, torch.full((3, 5000), 1 << 30, dtype=torch.int32, device="cuda")], 1)
+    b.check()
+    b.table = torch.cat([b.table, b.table[:2]])
+    b.total, b.start = b.total + [40, 0], np.concatenate([b.start, b.start[-1:], b.start[-1:]])
+    b.q = torch.cat([b.q] + [b.q[:2]] * 100)
+    b.check()
