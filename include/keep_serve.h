@@ -141,7 +141,8 @@ uint64_t keep_paged_attention_workspace_bytes(const keep_paged_cache* cache, int
 
 /*   q, out: DEVICE, 16-byte aligned, [n_rows] rows of [n_q_heads][head_dim]; they must not share an element (other columns of
  *     the same rows, with the same stride, are separate).
- *   q_start: DEVICE int32 [n_seqs + 1], not decreasing, within [0, n_rows] (clamped to that).
+ *   q_start: DEVICE int32 [n_seqs + 1], not decreasing, within [0, n_rows] (clamped to that).  A sequence whose end lies
+ *     before its start has no rows; what rows hold that two sequences claim is not defined.
  *   kv_len: DEVICE int32 [n_seqs] (clamped to [0, max_pages * page_size]).
  *   page_table: DEVICE int32 [n_seqs, max_pages]; entries behind a sequence's last page are not read, others are
  *     clamped to [0, n_pages).
