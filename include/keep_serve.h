@@ -166,7 +166,8 @@ keep_status keep_paged_attention(const keep_paged_attention_desc* desc, const ke
  * so that every sum below is exact, whatever its order.  Tokens are ranked by logit, equal logits by the lower id first.
  *   min_p: a token stays if w_i >= ceil(min_p 2^40);   top_k: and if it ranks among the first top_k of those;
  *   top_p: and if the weights ranked before it sum to less than ceil(top_p * (sum of what stays so far)).
- * The token is the first in rank whose weights up to and with its own exceed floor(u * (sum of what stays)).
+ * The token is the first in rank whose weights up to and with its own exceed floor(u * (sum of what stays)).  Both products
+ * with a sum are double arithmetic, from the sum rounded to double (sums beyond 2^53 lose their last bits there).
  * Logits of NaN, and of -infinity beside larger ones, weigh nothing; +infinity outweighs everything finite.  Temperatures of 0
  * and below (and NaN) choose the largest logit, the lowest id among equals.  A row without a number above -infinity gets token -1
  * and probability 0. */
