@@ -84,3 +84,19 @@ def test_what_the_order_of_sums_depends_on(dtype, fmt, dh):
     b.total, b.start = b.total + [40, 0], np.concatenate([b.start, b.start[-1:], b.start[-1:]])
     b.q = torch.cat([b.q] + [b.q[:2]] * 100)
     b.check()
+
+
+@pytest.mark.parametrize("dtype,fmt", [("f32", "f32"), ("bf16", "bf16")])
+def test_the_most_sequences_of_a_call(dtype, fmt):
+    r = np.random.default_rng(5)
+    b = Batch([(int(r.integers(0, 3)), int(r.integers(0, 40))) for _ in range(kb.KEEP_PAGED_MAX_SEQS)], 2, 1, 64, FORMATS[dtype], fmt, 8)
+    b.check()
+
+
+@pytest.mark.parametrize("dtype,fmt,dh", [("f32", "f32", 16), ("bf16", "bf16", 128), ("bf16", "int8", 64), ("bf16", "fp8", 256)])
+@pytest.mark.parametrize("hq,hkv", [(64, 1), (71, 1), (300, 2)])
+def test_many_heads_share_one(dtype, fmt, dh, hq, hkv):
+    """a token's rows fill several tiles, or end inside one"""
+    b = Batch([(1, 300), (3, 3), (2, 1), (0, 9), (5, 77)], hq, hkv, dh, FORMATS[dtype], fmt, 20, seed=hq)
+    b.check()
+    b.check(window=30)
