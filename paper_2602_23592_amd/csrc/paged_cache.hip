@@ -36,7 +36,7 @@ keep_status check_cache(const keep_paged_cache* c, const char* who) {
   const bool heads_inside = (H == 1 || c->head_stride >= W) && (T == 1 || c->token_stride >= (H - 1) * c->head_stride + W);
   const int64_t page = (T - 1) * c->token_stride + (H - 1) * c->head_stride + W;
   if ((!tokens_inside && !heads_inside) || (c->n_pages > 1 && c->page_stride < page))
-    return serve_fail(KEEP_ERR_INVALID_ARG, "%s: the cache's strides let tokens, heads or pages overlap", who);
+    return serve_fail(KEEP_ERR_INVALID_ARG, "%s: the cache's strides let tokens, heads or pages overlap, or a page reach past its stride", who);
   if (!c->k || !c->v) return serve_fail(KEEP_ERR_INVALID_ARG, "%s: the cache's k / v is NULL", who);
   if (!aligned16(c->k) || !aligned16(c->v))
     return serve_fail(KEEP_ERR_INVALID_ARG, "%s: the cache's k / v is not 16-byte aligned", who);
