@@ -97,9 +97,9 @@ typedef struct {
   int32_t head_dim; /* a multiple of 16, up to 256 */
   /* elements between pages, heads and tokens of k and of v (both laid out alike; a head's values are adjacent).  Each a
    * multiple of 16 bytes.  A page's values lie within its page_stride, its tokens and heads in either order.  Dense pages
-   * [n_kv_heads][page_size][head_dim] keep a head's tokens together, which reads
-   * fastest; the joined cache of a prefill, [tokens][n_kv_heads][head_dim], is the pages of token_stride = n_kv_heads *
-   * head_dim, head_stride = head_dim and page_stride = page_size * token_stride. */
+   * [n_kv_heads][page_size][head_dim] keep a head's tokens together, which reads fastest; the joined cache of a prefill,
+   * [tokens][n_kv_heads][head_dim], is the pages of token_stride = n_kv_heads * head_dim, head_stride = head_dim and
+   * page_stride = page_size * token_stride. */
   int64_t page_stride, head_stride, token_stride;
   void *k, *v;             /* DEVICE, 16-byte aligned */
   float *k_scale, *v_scale; /* DEVICE [n_pages][n_kv_heads][page_size]; 8-bit formats only, else NULL */

@@ -459,8 +459,8 @@ def rope_rows(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: t
 
 class PagedCache:
     """keep_paged_cache over tensors k, v [n_pages, n_kv_heads, page_size, head_dim] (float32, bfloat16, float8_e4m3fn or
-    int8; strides of 16-byte multiples, pages outermost, adjacent values) and, for the 8-bit types, float32 k_scale, v_scale [n_pages, n_kv_heads, page_size].
-    Keeps the tensors alive."""
+    int8; strides of 16-byte multiples, pages outermost, adjacent values) and, for the 8-bit types, float32 k_scale, v_scale
+    [n_pages, n_kv_heads, page_size].  Keeps the tensors alive."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
                  v_scale: Optional[torch.Tensor] = None):
