@@ -22,7 +22,7 @@
 // 8-bit codes become bf16 on their way into LDS, once for the four waves.
 // Eight chunks of 100 to 2000 tokens over up to 16k keys, 28 / 4 heads of 128, bf16 (589 GFLOP): 765 us and 23 for the join, 792
 // and 743 TFLOP/s a call, where a large product reaches 1419; 256 tokens over 33k int8 keys, 40 / 8 heads: 263 and 16, 269 a
-// call, 640 TFLOP/s (bf16 15 % more).  Boxes differ: 256 to 276 and 762 to 810 a call.  Exponentials and conversions share the
+// call, 640 TFLOP/s (bf16 15 % more).  Cards differ: 256 to 276 and 762 to 810 a call.  Exponentials and conversions share the
 // SIMD with the products, and 32 rows per wave feed each K and V operand to one product only.
 #include <type_traits>
 
